@@ -162,7 +162,7 @@ def prepare(case, seed):
             state["values"] = _in_blocks(state["values"], state["lengths"])
     if kind == "product" and own:
         from paper_1802_07170_amd import decoding
-        state["weight"] = decoding.QuantWeight.from_codes(state.pop("codes"), state.pop("scales"), case["group"])
+        state["weight"] = decoding.QuantWeight.from_codes(state.pop("codes").to(torch.uint8), state.pop("scales"), case["group"])
     if kind == "search":
         state["moved"] = [torch.zeros_like(t) for t in state["states"]]
     return state
