@@ -258,6 +258,70 @@ int cmt_wait_counts(cmt_handle* h, int64_t* loops, int64_t* again);
 
 const char* cmt_last_error(const cmt_handle* h);
 
+/* ---- Decoding in small numbers: operators on the caller's own tensors ----------------------------------------
+ * Products with 4-bit weights, attention over source rows held in 8 bits, a beam search's choice and the states that follow it: what one
+ * position of a search calls, for callers who drive the decoder themselves (cmt_quant_beam_decode below drives all of them).
+ * They need no handle.  Every call enqueues on hip_stream (NULL = the default stream) of the current device and returns: nothing is
+ * allocated, nothing waits, so all of them may be captured into a graph.  Buffers stay the caller's; a workspace is used by the call
+ * alone and holds nothing afterwards (calls that may run at the same time need one each).  Results do not depend on anything but the arguments: sums have a fixed order.
+ * cmt_operator_error gives the text of the calling thread's last refusal. */
+#define CMT_FP32 0
+#define CMT_BF16 1
+const char* cmt_operator_error(void);
+
+/* A weight [outputs, inputs] in 4 bits: W[n, k] = e2m1(code[n, k]) * scale[n, k / group], e2m1 of a code being {0, .5, 1, 1.5, 2, 3, 4,
+ * 6} of its lower three bits, negative with the fourth; scale in bf16; group 32, 64 or 128 (the last one of a row may be shorter).
+ * bytes: of the packed form, which is 256-byte aligned and laid out for the kernels: it is made by one of two calls,
+ *   cmt_quant_weight_pack    from a weight (row-major, pitch in elements): scale = bf16(max|w| / 6), the nearest codes (of two as near the
+ *                            even one).  A group with a value that is not finite gets the scale NaN, so that its products are NaN;
+ *   cmt_quant_weight_encode  from codes (row-major, one to a byte, the upper four bits ignored) and bf16 scales [outputs, ceil(inputs / group)];
+ * and cmt_quant_weight_values gives W in fp32, row-major.  1 <= outputs <= 2^24, 1 <= inputs <= 2^16, outputs * inputs <= 2^36. */
+int cmt_quant_weight_bytes(int32_t outputs, int32_t inputs, int32_t group, size_t* bytes);
+int cmt_quant_weight_pack(const void* weight_dev, int32_t type, int64_t pitch, int32_t outputs, int32_t inputs, int32_t group, void* packed_dev,
+                          void* hip_stream);
+int cmt_quant_weight_encode(const uint8_t* codes_dev, const uint16_t* scales_dev, int32_t outputs, int32_t inputs, int32_t group, void* packed_dev,
+                            void* hip_stream);
+int cmt_quant_weight_values(const void* packed_dev, int32_t outputs, int32_t inputs, int32_t group, float* weight_dev, void* hip_stream);
+/* y[m, n] = f(sum_k x[m, k] W[n, k] + bias[n]), f = tanh where tanh_of is not 0; bias_dev (fp32) may be NULL.  x of `type`, y of y_type (CMT_FP32
+ * or CMT_BF16), row-major with pitches in elements; 0 <= rows <= 65535 (0: nothing is done).  Products are exact, sums fp32 in either type. */
+int cmt_quant_product(const void* x_dev, int32_t type, int64_t x_pitch, int32_t rows, const void* packed_dev, int32_t outputs, int32_t inputs,
+                      int32_t group, const float* bias_dev, int32_t tanh_of, void* y_dev, int32_t y_type, int64_t y_pitch, void* hip_stream);
+
+/* Keys and values of up to max_tokens tokens of each sequence in 8 bits: whole numbers -127..127 times one fp32 scale for every 32 tokens of a
+ * sequence and head, keys and values apart: scale = max|x| / 127, code = x / scale to the nearest (of two the even one).
+ * sequences * heads <= 65535, 1 <= head_dim <= 1024, max_tokens <= 2^24; the cache is one buffer of `bytes`, 256-byte aligned. */
+typedef struct cmt_cache_config { int32_t sequences, heads, head_dim, max_tokens; } cmt_cache_config;
+int cmt_cache_bytes(const cmt_cache_config* cache, size_t* bytes);
+/* Where the elements of keys or values are: data[s * sequence_stride + t * token_stride + h * head_stride + d], strides in elements. */
+typedef struct cmt_cache_rows { const void* data_dev; int64_t sequence_stride, token_stride, head_stride; } cmt_cache_rows;
+/* Writes all sequences: tokens [0, lengths_dev[s]) of each, lengths clamped to [0, tokens]; they replace what was there.  What lies behind a
+ * sequence's length is not read.  A block with a value that is not finite gets the scale NaN.  1 <= tokens <= max_tokens. */
+int cmt_cache_fill(const cmt_cache_config* cache, void* cache_dev, const cmt_cache_rows* keys, const cmt_cache_rows* values, int32_t type,
+                   const int32_t* lengths_dev, int32_t tokens, void* hip_stream);
+/* The keys and values that a filled cache stands for: fp32 [sequences, tokens, heads, head_dim], 0 behind a sequence's length. */
+int cmt_cache_read(const cmt_cache_config* cache, const void* cache_dev, int32_t tokens, float* keys_dev, float* values_dev, void* hip_stream);
+/* out = sum_i a_i v_i, a = softmax over the tokens i below the sequence's length of scale * q.k_i; a sequence of length 0 gives 0.
+ * Row r [query_heads, head_dim] (heads side by side, row pitches in elements) belongs to sequence r / rows_per_sequence, r < sequences *
+ * rows_per_sequence; query head h reads key head h / (query_heads / heads).  tokens: no length may be larger (what is behind is not seen).  q and out of `type`; sums and the softmax are fp32. */
+int cmt_cache_attend_workspace(const cmt_cache_config* cache, int32_t rows_per_sequence, int32_t query_heads, int32_t tokens, size_t* bytes);
+int cmt_cache_attend(const cmt_cache_config* cache, const void* cache_dev, const void* query_dev, int32_t type, int64_t query_pitch,
+                     int32_t rows_per_sequence, int32_t query_heads, int32_t tokens, float scale, void* out_dev, int64_t out_pitch, void* workspace_dev,
+                     size_t workspace_bytes, void* hip_stream);
+
+/* The n best one-token extensions of each sentence's hypotheses: scores[b, s] + logits[b * beam + s, v] - log sum_v exp(logits[b * beam + s, v]),
+ * best first, of equal ones the lower (s, v).  logits of `type`, [sentences * beam, vocab] with a pitch in elements; scores fp32
+ * [sentences, beam], -inf for a place without a hypothesis (its logits are not read).  A logit of -inf is never taken; a row with a logit that
+ * is NaN or +inf, or whose score is no finite number, has no extensions.  Out, [sentences, n]: the scores in fp32, the row b * beam + s that is
+ * extended and the token; -inf, -1, -1 where there are fewer than n.  beam, n <= 32, vocab <= 2^26.  Scores are compared in 64 bits. */
+int cmt_beam_select_workspace(int32_t sentences, int32_t beam, int32_t vocab, size_t* bytes);
+int cmt_beam_select(const void* logits_dev, int32_t type, int64_t pitch, const float* scores_dev, int32_t sentences, int32_t beam, int32_t vocab,
+                    int32_t n, float* out_scores_dev, int32_t* out_rows_dev, int32_t* out_tokens_dev, void* workspace_dev, size_t workspace_bytes,
+                    void* hip_stream);
+/* target[r] = source[rows[r]] for r < count, of n tensors of rows of row_bytes (pitches in bytes; `tensors` is host memory, read before the call
+ * returns).  A row whose number is outside [0, source_rows) is left as it was.  No target may overlap a source or another target. */
+typedef struct cmt_reorder_tensor { const void* source_dev; void* target_dev; int64_t source_pitch, target_pitch, row_bytes; } cmt_reorder_tensor;
+int cmt_beam_reorder(const int32_t* rows_dev, int32_t count, int32_t source_rows, const cmt_reorder_tensor* tensors, int32_t n, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

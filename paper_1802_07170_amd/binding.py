@@ -19,6 +19,9 @@ EXPORTS = [
     "cmt_fetch_loss", "cmt_get_grads", "cmt_sgd_update", "cmt_debug_fetch", "cmt_padded_batch",
     "cmt_time_kernel", "cmt_last_error", "cmt_set_regularization", "cmt_greedy_decode", "cmt_beam_decode",
     "cmt_eval_loss", "cmt_eval_loss_static", "cmt_wait_counts",
+    "cmt_operator_error", "cmt_quant_weight_bytes", "cmt_quant_weight_pack", "cmt_quant_weight_encode",
+    "cmt_quant_weight_values", "cmt_quant_product", "cmt_cache_bytes", "cmt_cache_fill", "cmt_cache_read",
+    "cmt_cache_attend_workspace", "cmt_cache_attend", "cmt_beam_select_workspace", "cmt_beam_select", "cmt_beam_reorder",
 ]
 
 
@@ -26,6 +29,18 @@ class CmtConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in (
         "src_vocab", "tgt_vocab", "emb_dim", "hidden", "layers", "max_batch", "max_src_len",
         "max_tgt_len", "precision", "bos_id", "pad_id")]
+
+
+class CmtCacheConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("sequences", "heads", "head_dim", "max_tokens")]
+
+
+class CmtCacheRows(C.Structure):
+    _fields_ = [("data", C.c_void_p)] + [(n, C.c_int64) for n in ("sequence_stride", "token_stride", "head_stride")]
+
+
+class CmtReorderTensor(C.Structure):
+    _fields_ = [("source", C.c_void_p), ("target", C.c_void_p)] + [(n, C.c_int64) for n in ("source_pitch", "target_pitch", "row_bytes")]
 
 
 class CmtError(RuntimeError):
@@ -75,8 +90,24 @@ def load_library():
     lib.cmt_wait_counts.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
     lib.cmt_last_error.argtypes = [vp]
     lib.cmt_last_error.restype = C.c_char_p
+    i64, szp, cachep, rowsp = C.c_int64, C.POINTER(sz), C.POINTER(CmtCacheConfig), C.POINTER(CmtCacheRows)
+    lib.cmt_operator_error.argtypes = []
+    lib.cmt_operator_error.restype = C.c_char_p
+    lib.cmt_quant_weight_bytes.argtypes = [i32, i32, i32, szp]
+    lib.cmt_quant_weight_pack.argtypes = [vp, i32, i64, i32, i32, i32, vp, vp]
+    lib.cmt_quant_weight_encode.argtypes = [vp, vp, i32, i32, i32, vp, vp]
+    lib.cmt_quant_weight_values.argtypes = [vp, i32, i32, i32, vp, vp]
+    lib.cmt_quant_product.argtypes = [vp, i32, i64, i32, vp, i32, i32, i32, vp, i32, vp, i32, i64, vp]
+    lib.cmt_cache_bytes.argtypes = [cachep, szp]
+    lib.cmt_cache_fill.argtypes = [cachep, vp, rowsp, rowsp, i32, vp, i32, vp]
+    lib.cmt_cache_read.argtypes = [cachep, vp, i32, vp, vp, vp]
+    lib.cmt_cache_attend_workspace.argtypes = [cachep, i32, i32, i32, szp]
+    lib.cmt_cache_attend.argtypes = [cachep, vp, vp, i32, i64, i32, i32, i32, C.c_float, vp, i64, vp, sz, vp]
+    lib.cmt_beam_select_workspace.argtypes = [i32, i32, i32, szp]
+    lib.cmt_beam_select.argtypes = [vp, i32, i64, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.cmt_beam_reorder.argtypes = [vp, i32, i32, C.POINTER(CmtReorderTensor), i32, vp]
     for name in EXPORTS:
-        if name not in ("cmt_destroy", "cmt_last_error"):
+        if name not in ("cmt_destroy", "cmt_last_error", "cmt_operator_error"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib

@@ -1,0 +1,400 @@
+// Source rows in 8 bits and the attention that reads them: keys and values of every block of 32 tokens and head as whole numbers of
+// -127..127 times one fp32 scale each.
+//
+// o = sum_i a_i v_i, a = softmax over the tokens i below the sequence's length of scale q.k_i.  The codes are exact in bf16, so
+// both products run on the bf16 matrix instructions: the queries as they are (fp32 ones as three bf16 parts), the weights
+// a_i (times the values' scale) as two (three) bf16 parts; sums, maxima and scales are fp32.
+// Every query of a sequence and key head shares its tokens' bytes: 2 D bytes a token for 4 D flop a query.  The read bounds it.
+#include <algorithm>
+#include <type_traits>
+
+#include "lowbit.h"
+
+namespace cmt {
+
+// Nearest whole number to x / s, the even one of two, as if the quotient were exact.  inv ~ 1 / s.
+__device__ __forceinline__ float cache_code(float x, float s, float inv) {
+  float q = rintf(x * inv);
+  const float r = fmaf(-q, s, x), r2 = 2.f * fabsf(r);       // (exact: |r| < 2 s and a multiple of half an ulp of s)
+  if (r2 > s || (r2 == s && ((int)q & 1))) q += copysignf(1.f, r);
+  return fminf(fmaxf(q, -127.f), 127.f);
+}
+
+// ---- writing ---------------------------------------------------------------------------------------------
+constexpr int FILL_PAD = 16;
+template <typename T>
+__device__ __forceinline__ void fill_load(const T* p, int n, bool wide, float (&x)[16]) {
+  if (n >= 16 && wide) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      Frag<T> f;
+      f.load(p + 8 * h);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[8 * h + i] = f.get(i);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = i < n ? to_f(p[i]) : 0.f;
+  }
+}
+// One workgroup per block of 32 tokens, sequence and head; blockIdx.z: keys, values.
+template <typename T>
+__global__ __launch_bounds__(256) void cache_fill_kernel(CacheSource src, const int32_t* __restrict__ lengths, int tokens, CacheShape s, CacheView c, int wide) {
+  __shared__ __align__(16) int8_t code[CACHE_BLOCK * (1024 + FILL_PAD)];
+  __shared__ float s_most[4];
+  __shared__ int s_bad[4];
+  const int b = blockIdx.y / s.heads, head = blockIdx.y % s.heads, blk = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const bool is_v = blockIdx.z;
+  const int len = min(max(lengths[b], 0), tokens);
+  if (t == 0 && head == 0 && blk == 0 && !is_v) c.lengths[b] = len;
+  const int n = min(len - blk * CACHE_BLOCK, CACHE_BLOCK);   // valid tokens of the block
+  if (n <= 0) return;                                        // (nothing reads it)
+  const size_t tok = is_v ? src.v_tok : src.k_tok;
+  const T* p = (const T*)(is_v ? src.v : src.k) + (size_t)b * (is_v ? src.v_seq : src.k_seq) + (size_t)head * (is_v ? src.v_head : src.k_head) +
+               (size_t)blk * CACHE_BLOCK * tok;
+  const int chunks = s.chunks(), ld = chunks * 64 + FILL_PAD, slots = chunks * 128;   // a slot: 16 d of a token
+  const bool wd = wide >> is_v & 1;
+  float x[16], most = 0.f;
+  bool bad = false;
+  for (int i = t; i < slots; i += 256) {
+    const int r = (i & 15) + 16 * (i >> 6 & 1), d = 64 * (i >> 7) + 16 * (i >> 4 & 3);
+    if (r >= n || d >= s.dim) continue;
+    fill_load(p + (size_t)r * tok + d, s.dim - d, wd, x);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) { most = fmaxf(most, fabsf(x[e])); bad |= !(fabsf(x[e]) <= 3.4028235e38f); }
+  }
+  most = wave_max(most);
+  const bool any = __ballot(bad) != 0;
+  if (lane == 0) { s_most[w] = most; s_bad[w] = any; }
+  __syncthreads();
+  most = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
+  const bool finite = !(s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3]);
+  const float scale = finite ? most / 127.0f : __uint_as_float(0x7fc00000u);   // (a block with a number that is none: no result hides it)
+  const size_t at = ((size_t)b * s.heads + head) * s.blocks() + blk;
+  if (t == 0) (is_v ? c.vscale : c.kscale)[at] = scale;
+  const bool some = scale > 0.f, tiny = scale < 1e-36f;
+  const float inv = 1.0f / scale;
+  for (int i = t; i < slots; i += 256) {
+    const int r = (i & 15) + 16 * (i >> 6 & 1), d = 64 * (i >> 7) + 16 * (i >> 4 & 3);
+    uint32_t o[4] = {0, 0, 0, 0};
+    if (some && r < n && d < s.dim) {
+      fill_load(p + (size_t)r * tok + d, s.dim - d, wd, x);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int q = tiny ? (int)fmin(fmax(rint((double)x[e] / (double)scale), -127.0), 127.0) : (int)cache_code(x[e], scale, inv);
+        o[e >> 2] |= (uint32_t)(q & 255) << (8 * (e & 3));
+      }
+    }
+    *reinterpret_cast<uint4*>(code + r * ld + d) = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+  __syncthreads();
+  char* out = (is_v ? c.v : c.k) + at * chunks * 2048;
+  if (!is_v) {
+    for (int i = t; i < slots; i += 256) {                   // [16-token tile][chunk][lane]
+      const int tile = i / (chunks * 64), rest = i - tile * chunks * 64, ch = rest >> 6, l = rest & 63;
+      *reinterpret_cast<uint4*>(out + (size_t)i * 16) = *reinterpret_cast<const uint4*>(code + (16 * tile + (l & 15)) * ld + 64 * ch + 16 * (l >> 4));
+    }
+  } else {
+    for (int i = t; i < slots; i += 256) {                   // [32 d][lane]
+      const int l = i & 63, d = 32 * (i >> 6) + (l & 15), r = 4 * (l >> 4);
+      uint32_t o[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int8_t* q = code + (r + 16 * (k & 1)) * ld + d + 16 * (k >> 1);
+        o[k] = (uint32_t)(uint8_t)q[0] | (uint32_t)(uint8_t)q[ld] << 8 | (uint32_t)(uint8_t)q[2 * ld] << 16 | (uint32_t)(uint8_t)q[3 * ld] << 24;
+      }
+      *reinterpret_cast<uint4*>(out + (size_t)i * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+  }
+}
+void launch_cache_fill(int prec, const CacheSource& src, const int32_t* lengths, int tokens, const CacheShape& s, void* cache, hipStream_t st) {
+  const size_t es = prec ? 2 : 4;
+  auto wide = [&](const void* p, size_t a, size_t b, size_t c) { return (((uintptr_t)p | a * es | b * es | c * es) & 15) == 0; };
+  const int flags = (wide(src.k, src.k_seq, src.k_tok, src.k_head) ? 1 : 0) | (wide(src.v, src.v_seq, src.v_tok, src.v_head) ? 2 : 0);
+  const dim3 grid((unsigned)std::max(1, (tokens + CACHE_BLOCK - 1) / CACHE_BLOCK), (unsigned)(s.seqs * s.heads), 2);
+  if (prec) hipLaunchKernelGGL(cache_fill_kernel<bf16_t>, grid, dim3(256), 0, st, src, lengths, tokens, s, CacheView(s, cache), flags);
+  else hipLaunchKernelGGL(cache_fill_kernel<float>, grid, dim3(256), 0, st, src, lengths, tokens, s, CacheView(s, cache), flags);
+}
+
+// ---- reading back: [seqs, tokens, heads, dim], 0 behind a sequence's end -------------------------------------
+__global__ __launch_bounds__(256) void cache_read_kernel(CacheShape s, CacheView c, int tokens, float* __restrict__ k, float* __restrict__ v) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, n = (size_t)s.seqs * tokens * s.heads * s.dim;
+  if (i >= n) return;
+  float* const out = blockIdx.y ? v : k;
+  const int d = (int)(i % s.dim);
+  size_t r = i / s.dim;
+  const int head = (int)(r % s.heads);
+  r /= s.heads;
+  const int t = (int)(r % tokens), b = (int)(r / tokens);
+  float x = 0.f;
+  if (t < c.lengths[b]) {
+    const size_t at = ((size_t)b * s.heads + head) * s.blocks() + (t >> 5);
+    const char* base = (blockIdx.y ? c.v : c.k) + at * s.chunks() * 2048;
+    const int q = t & 15, hi = t >> 4 & 1;
+    const size_t off = blockIdx.y ? (size_t)(d >> 5) * 1024 + ((q >> 2) * 16 + (d & 15)) * 16 + 8 * (d >> 4 & 1) + 4 * hi + (q & 3)
+                                  : ((size_t)hi * s.chunks() + (d >> 6)) * 1024 + ((d >> 4 & 3) * 16 + q) * 16 + (d & 15);
+    x = (float)(int8_t)base[off] * (blockIdx.y ? c.vscale : c.kscale)[at];
+  }
+  out[i] = x;
+}
+void launch_cache_read(const CacheShape& s, const void* cache, int tokens, float* k, float* v, hipStream_t st) {
+  const size_t n = (size_t)s.seqs * tokens * s.heads * s.dim;
+  hipLaunchKernelGGL(cache_read_kernel, dim3((unsigned)((n + 255) / 256), 2), dim3(256), 0, st, s, CacheView(s, const_cast<void*>(cache)), tokens, k, v);
+}
+
+// ---- the attention -------------------------------------------------------------------------------------------
+// 8 codes -> operand of 8 bf16 (exact)
+__device__ __forceinline__ void cache_operand(uint32_t a, uint32_t b, Frag<bf16_t>& f) {
+  auto two = [](uint32_t w, int sh) {
+    const float x = (float)(int8_t)(w >> sh), y = (float)(int8_t)(w >> (sh + 8));
+    return pack_hi(__float_as_uint(x), __float_as_uint(y));
+  };
+  f.v = make_uint4(two(a, 0), two(a, 16), two(b, 0), two(b, 16));
+}
+
+constexpr int ATTEND_WAVES = 8, ATTEND_CHUNK = 128, ATTEND_LD = ATTEND_CHUNK + 4;
+struct AttendPlan { int g_tiles, splits, per_split; };      // tiles of 16 queries; ranges of the tokens, of so many chunks of 128
+static AttendPlan attend_plan(const CacheShape& s, int per, int q_heads, int tokens) {
+  AttendPlan p;
+  p.g_tiles = (per * (q_heads / s.heads) + 15) / 16;
+  const long units = (long)s.seqs * s.heads * p.g_tiles;
+  const int chunks = std::max(1, (tokens + ATTEND_CHUNK - 1) / ATTEND_CHUNK);
+  const int want = (int)std::min<long>(chunks, std::max<long>(1, 512 / units));
+  p.per_split = (chunks + want - 1) / want;
+  p.splits = (chunks + p.per_split - 1) / p.per_split;
+  return p;
+}
+size_t cache_attend_workspace(const CacheShape& s, int per, int q_heads, int tokens) {
+  const AttendPlan p = attend_plan(s, per, q_heads, tokens);
+  if (p.splits == 1) return 0;
+  return (size_t)s.seqs * s.heads * p.g_tiles * p.splits * 16 * (2 + (size_t)s.chunks() * 64) * 4;
+}
+
+struct AttendArgs {
+  const void* q; size_t ldq; void* out; size_t ldo;
+  int per, share, splits, per_split, tokens, wide_q, wide_o;
+  float scale;
+  float* ml; float* part;                                    // of splits: (maximum, sum) [unit][split][16], products [unit][split][16][64 chunks]
+};
+// A workgroup takes one tile of 16 queries of a sequence and key head through a range of its tokens, 128 at a time: its wavefronts
+// make the scores of 16 tokens each, then the weights together, then each the products of 32 EPW (of few d: of some of the tokens)
+// columns of the values.
+template <typename T, int EPW>
+__global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendArgs a, CacheShape s, CacheView c) {
+  constexpr int QP = OPERAND_PARTS<T>, PP = QP + (QP == 1);
+  constexpr bool FAST = sizeof(T) == 2;
+  __shared__ uint4 s_q[8 * EPW * QP * 64];
+  __shared__ __align__(16) float s_s[16 * ATTEND_LD];
+  __shared__ __align__(16) uint4 s_p[4 * PP * 64];
+  __shared__ float s_f[16], s_l[16], s_m[16];
+  const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int split = blockIdx.x % a.splits;
+  int u = blockIdx.x / a.splits;
+  const int unit = u, G = a.per * a.share, g_tiles = (G + 15) / 16;
+  const int g0 = (u % g_tiles) * 16; u /= g_tiles;
+  const int head = u % s.heads, b = u / s.heads;
+  const int len = min(c.lengths[b], a.tokens);
+  const int chunks = s.chunks(), E = chunks * 2;
+  const int first = split * a.per_split * ATTEND_CHUNK, last = min(len, first + a.per_split * ATTEND_CHUNK);
+  const size_t at = ((size_t)b * s.heads + head) * s.blocks();
+  const char* const kc = c.k + at * chunks * 2048;
+  const char* const vc = c.v + at * chunks * 2048;
+  const int q4 = lane >> 4, g = lane & 15;
+  auto query = [&](int i) { return ((size_t)b * a.per + (g0 + i) / a.share); };   // row of query i of the tile
+  auto column = [&](int i) { return (size_t)(head * a.share + (g0 + i) % a.share) * s.dim; };
+  if (first < last)
+    for (int i = t; i < chunks * 128; i += 64 * ATTEND_WAVES) {   // the queries as operands: [chunk][half][part][lane]
+      const int l = i & 63, ch = i >> 7, h = i >> 6 & 1, d = 64 * ch + 16 * (l >> 4) + 8 * h;
+      Frag<bf16_t> f[QP];
+      const bool in = g0 + (l & 15) < G && d < s.dim;
+      load_operand((const T*)a.q + (in ? query(l & 15) * a.ldq + column(l & 15) + d : 0), in ? s.dim - d : 0, a.wide_q, f);
+#pragma unroll
+      for (int p = 0; p < QP; ++p) s_q[((ch * 2 + h) * QP + p) * 64 + l] = f[p].v;
+    }
+  const int ts = E >= 6 ? 1 : 8 / E, mine = E >= 6 ? w * EPW : w % E, my_ts = E >= 6 ? 0 : w / E;   // columns 32 mine.., tokens' share
+  v4f acc[EPW][2];
+#pragma unroll
+  for (int e = 0; e < EPW; ++e) acc[e][0] = acc[e][1] = v4f{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;                              // of query t / 32, in its 32 threads
+  __syncthreads();
+  for (int t0 = first; t0 < last; t0 += ATTEND_CHUNK) {
+    const int tile = t0 + 16 * w;
+    if (tile < last) {
+      const uint4* kp = reinterpret_cast<const uint4*>(kc + (size_t)(tile >> 4) * chunks * 1024) + lane;
+      v4f z[2] = {v4f{0.f, 0.f, 0.f, 0.f}, v4f{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll 4
+      for (int ch = 0; ch < chunks; ++ch) {
+        const uint4 k = kp[ch * 64];
+        Frag<bf16_t> k0, k1, qf;
+        cache_operand(k.x, k.y, k0);
+        cache_operand(k.z, k.w, k1);
+#pragma unroll
+        for (int p = QP - 1; p >= 0; --p) {
+          qf.v = s_q[(ch * 2 * QP + p) * 64 + lane]; mma16(z[0], k0, qf);
+          qf.v = s_q[((ch * 2 + 1) * QP + p) * 64 + lane]; mma16(z[1], k1, qf);
+        }
+      }
+      const float sc = c.kscale[at + (tile >> 5)] * a.scale;
+      *reinterpret_cast<float4*>(s_s + g * ATTEND_LD + 16 * w + 4 * q4) =
+          make_float4((z[0][0] + z[1][0]) * sc, (z[0][1] + z[1][1]) * sc, (z[0][2] + z[1][2]) * sc, (z[0][3] + z[1][3]) * sc);
+    }
+    __syncthreads();
+    {
+      const int i = t >> 5, j = t & 31, tok = t0 + 4 * j;
+      const float4 x4 = *reinterpret_cast<const float4*>(s_s + i * ATTEND_LD + 4 * j);
+      float x[4] = {x4.x, x4.y, x4.z, x4.w}, mx = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) if (tok + e < last) mx = fmaxf(mx, x[e]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+      const float mn = fmaxf(m, mx), ms = mn > -INFINITY ? mn : 0.f;
+      const float f = m > -INFINITY ? (FAST ? __expf(m - ms) : expf(m - ms)) : 0.f;
+      const float vs = tok < last ? c.vscale[at + (tok >> 5)] : 0.f;
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = tok + e < last ? (FAST ? __expf(x[e] - ms) : expf(x[e] - ms)) : 0.f;
+        sum += x[e];
+        x[e] = tok + e < last ? x[e] * vs : 0.f;
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      l = l * f + sum;
+      m = mn;
+      if (j == 0) s_f[i] = f;
+      // as an operand: token 4 c + e of the block's first half in slots 0..3 of quarter c, of its second half in slots 4..7
+      uint2* const to = reinterpret_cast<uint2*>(s_p) + ((j >> 3) * PP * 64 + (j & 3) * 16 + i) * 2 + (j >> 2 & 1);
+      if (PP == 2) {
+        const uint32_t h0 = f2bf(x[0]), h1 = f2bf(x[1]), h2 = f2bf(x[2]), h3 = f2bf(x[3]);
+        to[0] = make_uint2(h0 | h1 << 16, h2 | h3 << 16);
+        const uint32_t l0 = f2bf(x[0] - bf2f((bf16_t)h0)), l1 = f2bf(x[1] - bf2f((bf16_t)h1)), l2 = f2bf(x[2] - bf2f((bf16_t)h2)),
+                       l3 = f2bf(x[3] - bf2f((bf16_t)h3));
+        to[128] = make_uint2(l0 | l1 << 16, l2 | l3 << 16);
+      } else {
+        const Parts3 a0 = parts3(x[0]), a1 = parts3(x[1]), a2 = parts3(x[2]), a3 = parts3(x[3]);
+        to[0] = make_uint2(pack_hi(a0.h, a1.h), pack_hi(a2.h, a3.h));
+        to[128] = make_uint2(pack_hi(a0.m, a1.m), pack_hi(a2.m, a3.m));
+        to[256] = make_uint2(pack_hi(a0.l, a1.l), pack_hi(a2.l, a3.l));
+      }
+    }
+    __syncthreads();
+    const float f = s_f[g];
+#pragma unroll
+    for (int e = 0; e < EPW; ++e)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[e][h][i] *= f;
+    for (int blk = my_ts; blk < ATTEND_CHUNK / CACHE_BLOCK; blk += ts) {
+      if (t0 + blk * CACHE_BLOCK >= last) break;
+      const uint4* vp = reinterpret_cast<const uint4*>(vc + (size_t)((t0 >> 5) + blk) * chunks * 2048) + lane;
+      Frag<bf16_t> pf[PP];
+#pragma unroll
+      for (int p = 0; p < PP; ++p) pf[p].v = s_p[(blk * PP + p) * 64 + lane];
+#pragma unroll
+      for (int e = 0; e < EPW; ++e)
+        if (mine + e < E) {
+          const uint4 v = vp[(mine + e) * 64];
+          Frag<bf16_t> v0, v1;
+          cache_operand(v.x, v.y, v0);
+          cache_operand(v.z, v.w, v1);
+#pragma unroll
+          for (int p = PP - 1; p >= 0; --p) { mma16(acc[e][0], v0, pf[p]); mma16(acc[e][1], v1, pf[p]); }
+        }
+    }
+  }
+  if ((t & 31) == 0) { s_m[t >> 5] = m; s_l[t >> 5] = l; }
+  if (ts > 1) {                                              // the tokens' shares of the same columns (E is 2 or 4: EPW is 1)
+    __syncthreads();                                         // (also: the last weights have been read)
+    float4* const red = reinterpret_cast<float4*>(s_q);      // 8 KB x QP: [wavefront][half][lane] is 16 KB where ts is 4 or 2
+    // wavefronts of the upper shares hand over in turn, so that two halves of one wavefront's 2 KB fit
+    for (int k = 1; k < ts; ++k) {
+      if (my_ts == k) { red[(mine * 2) * 64 + lane] = make_float4(acc[0][0][0], acc[0][0][1], acc[0][0][2], acc[0][0][3]);
+                        red[(mine * 2 + 1) * 64 + lane] = make_float4(acc[0][1][0], acc[0][1][1], acc[0][1][2], acc[0][1][3]); }
+      __syncthreads();
+      if (my_ts == 0)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 x = red[(mine * 2 + h) * 64 + lane];
+          acc[0][h][0] += x.x; acc[0][h][1] += x.y; acc[0][h][2] += x.z; acc[0][h][3] += x.w;
+        }
+      __syncthreads();
+    }
+    if (my_ts) return;
+  } else
+    __syncthreads();
+  if (a.splits > 1) {
+    const size_t slot = (size_t)unit * a.splits + split;
+    if (t < 16) { a.ml[(slot * 16 + t) * 2] = s_m[t]; a.ml[(slot * 16 + t) * 2 + 1] = s_l[t]; }
+    if (first >= last) return;
+    float* part = a.part + (slot * 16 + g) * chunks * 64;
+#pragma unroll
+    for (int e = 0; e < EPW; ++e)
+      if (mine + e < E)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          *reinterpret_cast<float4*>(part + 32 * (mine + e) + 16 * h + 4 * q4) = make_float4(acc[e][h][0], acc[e][h][1], acc[e][h][2], acc[e][h][3]);
+    return;
+  }
+  if (g0 + g >= G) return;
+  const float sum = s_l[g], inv = sum == 0.f ? 0.f : 1.0f / sum;
+  T* const out = (T*)a.out + query(g) * a.ldo + column(g);
+#pragma unroll
+  for (int e = 0; e < EPW; ++e)
+    if (mine + e < E)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int d = 32 * (mine + e) + 16 * h + 4 * q4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (d + i < s.dim) out[d + i] = from_f<T>(acc[e][h][i] * inv);
+      }
+}
+// joins the ranges of a query: one workgroup each
+template <typename T>
+__global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a, CacheShape s) {
+  const int G = a.per * a.share, g_tiles = (G + 15) / 16;
+  int u = blockIdx.x;
+  const int g = u % G; u /= G;
+  const int head = u % s.heads, b = u / s.heads;
+  const size_t slot = ((size_t)(b * s.heads + head) * g_tiles + g / 16) * a.splits;
+  const float* ml = a.ml + (slot * 16 + g % 16) * 2;
+  float M = -INFINITY, L = 0.f;
+  for (int k = 0; k < a.splits; ++k) M = fmaxf(M, ml[k * 32]);
+  const float Ms = M > -INFINITY ? M : 0.f;
+  for (int k = 0; k < a.splits; ++k) if (ml[k * 32 + 1] != 0.f) L += ml[k * 32 + 1] * expf(ml[k * 32] - Ms);
+  const float inv = L == 0.f ? 0.f : 1.0f / L;
+  T* const out = (T*)a.out + ((size_t)b * a.per + g / a.share) * a.ldo + (size_t)(head * a.share + g % a.share) * s.dim;
+  const size_t ld = (size_t)s.chunks() * 64;
+  for (int d = threadIdx.x; d < s.dim; d += 256) {
+    float o = 0.f;
+    for (int k = 0; k < a.splits; ++k) if (ml[k * 32 + 1] != 0.f) o += a.part[((slot + k) * 16 + g % 16) * ld + d] * expf(ml[k * 32] - Ms);
+    out[d] = from_f<T>(o * inv);
+  }
+}
+void launch_cache_attend(int prec, const CacheShape& s, const void* cache, const void* q, size_t ldq, int per, int q_heads, int tokens, float scale,
+                         void* out, size_t ldo, void* workspace, hipStream_t st) {
+  const AttendPlan p = attend_plan(s, per, q_heads, tokens);
+  const size_t es = prec ? 2 : 4;
+  const long units = (long)s.seqs * s.heads * p.g_tiles;
+  AttendArgs a{};
+  a.q = q; a.ldq = ldq; a.out = out; a.ldo = ldo; a.per = per; a.share = q_heads / s.heads; a.splits = p.splits; a.per_split = p.per_split;
+  a.tokens = tokens; a.scale = scale;
+  a.wide_q = (((uintptr_t)q | ldq * es | s.dim * es) & 15) == 0;
+  a.ml = (float*)workspace; a.part = a.ml + (size_t)units * p.splits * 32;
+  auto go = [&](auto type, auto epw) {
+    using T = decltype(type);
+    hipLaunchKernelGGL((cache_attend_kernel<T, decltype(epw)::value>), dim3((unsigned)(units * p.splits)), dim3(64 * ATTEND_WAVES), 0, st, a, s,
+                       CacheView(s, const_cast<void*>(cache)));
+    if (p.splits > 1) hipLaunchKernelGGL(cache_join_kernel<T>, dim3((unsigned)((long)s.seqs * s.heads * per * a.share)), dim3(256), 0, st, a, s);
+  };
+  auto by_width = [&](auto type) {
+    const int chunks = s.chunks();
+    if (chunks <= 4) go(type, std::integral_constant<int, 1>());
+    else if (chunks <= 8) go(type, std::integral_constant<int, 2>());
+    else go(type, std::integral_constant<int, 4>());
+  };
+  if (prec) by_width(bf16_t{}); else by_width(float{});
+}
+
+}  // namespace cmt

@@ -1,0 +1,135 @@
+// Launchers of the kernels for decoding in small numbers (quant.hip, cache.hip, search.hip) and what they share.  As in kernels.h: they
+// only enqueue work on `st`; none allocates or synchronises.  `prec`: 0 = float, 1 = bf16 (raw uint16).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "common.h"
+
+namespace cmt {
+
+// ---- quant.hip: products with 4-bit weights ---------------------------------------------------------
+// A weight [N, K] is held as e2m1 codes (the format that the hardware turns into bf16, two to an instruction) in tiles of 16 rows x 128 k:
+// 1 KB, lane l's 16 bytes being row l % 16, of which dword s holds k = 32 s + 8 (l / 16) + 0..7 (low nibble first) - the register
+// operand of the 16x16x32 matrix instruction.  Tiles of a row block follow each other in k; rows and k beyond the matrix are 0.
+// Behind the codes: bf16 scales [row block][k / group][16 rows], 0 beyond the matrix.
+constexpr int QUANT_TILE_K = 128;
+struct QuantShape {
+  int N, K, group;
+  __host__ __device__ int row_blocks() const { return (N + 15) / 16; }
+  __host__ __device__ int k_tiles() const { return (K + QUANT_TILE_K - 1) / QUANT_TILE_K; }
+  size_t code_bytes() const { return (size_t)row_blocks() * k_tiles() * 1024; }
+  size_t scale_bytes() const { return (size_t)row_blocks() * k_tiles() * (QUANT_TILE_K / group) * 32; }
+  size_t bytes() const { return (code_bytes() + scale_bytes() + 255) & ~(size_t)255; }
+};
+struct QuantWeightRef { QuantShape shape; const char* packed; };
+void launch_quant_pack(int prec, const void* w, size_t ldw, const QuantShape& q, void* packed, hipStream_t st);
+void launch_quant_encode(const uint8_t* codes, const bf16_t* scales, const QuantShape& q, void* packed, hipStream_t st);
+void launch_quant_values(const void* packed, const QuantShape& q, float* out, hipStream_t st);
+// y [M, N] = f(x [M, K] W^T + bias), f = tanh or nothing; x of type prec, y of type y_prec; bias fp32 or null.
+void launch_quant_product(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, bool tanh, int y_prec, void* y,
+                          size_t ldy, hipStream_t st);
+
+// ---- cache.hip: source rows in 8 bits -------------------------------------------------------------
+// Per (sequence, head, block of 32 tokens) one fp32 scale for the keys and one for the values; codes are whole numbers -127..127.
+// Keys: tiles of 16 tokens x 64 d, 1 KB, lane l's 16 bytes being token l % 16, d = 16 (l / 16) + 0..15.
+// Values: tiles of 32 tokens x 32 d, 1 KB, lane l's bytes 8 h + j (h = 0, 1) being d = 16 h + l % 16 and token 4 (l / 16) + j (j < 4)
+// or 12 + 4 (l / 16) + j: the order in which the scores' accumulators hold the tokens, so that weights go from one
+// product into the other without leaving their lanes.
+constexpr int CACHE_BLOCK = 32;
+struct CacheShape {
+  int seqs, heads, dim, tokens;                            // tokens: the capacity
+  __host__ __device__ int blocks() const { return (tokens + CACHE_BLOCK - 1) / CACHE_BLOCK; }
+  __host__ __device__ int chunks() const { return (dim + 63) / 64; }           // of 64 d
+  size_t part() const { return (size_t)seqs * heads * blocks(); }
+  size_t lengths_bytes() const { return ((size_t)seqs * 4 + 255) & ~(size_t)255; }
+  size_t scales_bytes() const { return (part() * 4 + 255) & ~(size_t)255; }
+  size_t codes_bytes() const { return part() * chunks() * 2048; }
+  size_t bytes() const { return lengths_bytes() + 2 * scales_bytes() + 2 * codes_bytes(); }
+};
+struct CacheView {
+  int32_t* lengths; float *kscale, *vscale; char *k, *v;
+  CacheView(const CacheShape& s, void* base) {
+    char* p = (char*)base;
+    lengths = (int32_t*)p; p += s.lengths_bytes();
+    kscale = (float*)p; p += s.scales_bytes();
+    vscale = (float*)p; p += s.scales_bytes();
+    k = p; p += s.codes_bytes();
+    v = p;
+  }
+};
+struct CacheSource { const void *k, *v; size_t k_seq, k_tok, k_head, v_seq, v_tok, v_head; };   // strides in elements; d contiguous
+void launch_cache_fill(int prec, const CacheSource& src, const int32_t* lengths, int tokens, const CacheShape& s, void* cache, hipStream_t st);
+void launch_cache_read(const CacheShape& s, const void* cache, int tokens, float* k, float* v, hipStream_t st);
+// Attention of rows x q_heads queries; row r belongs to sequence r / per.  q, out: [rows, q_heads, dim] with row pitches, heads side by side.
+size_t cache_attend_workspace(const CacheShape& s, int per, int q_heads, int tokens);
+void launch_cache_attend(int prec, const CacheShape& s, const void* cache, const void* q, size_t ldq, int per, int q_heads, int tokens, float scale,
+                         void* out, size_t ldo, void* workspace, hipStream_t st);
+
+// ---- search.hip: a beam search's choice --------------------------------------------------------------
+constexpr int SEARCH_MAX = 32, SEARCH_GROUP = 512;
+constexpr int SEARCH_MAX_VOCAB = 1 << 26;
+// What a search that is kept on the device does with the best extensions (the rules of cmt_beam_decode): those that end leave the
+// beam, the others fill its places, best first.  Rows beyond R and lists as in BeamState.
+struct SearchAdvance {
+  int32_t *hist_tok, *hist_par, *nlive, *fin_step, *fin_par, *fin_tok; float* fin_score;
+  int hist_ld, j, max_len, eos; float alpha;
+};
+size_t search_workspace(int B, int K, int V);
+void launch_search_select(int prec, const void* logits, size_t ld, const float* scores, int B, int K, int V, int n, float* out_scores,
+                          int32_t* out_rows, int32_t* out_tokens, const SearchAdvance* adv, void* workspace, hipStream_t st);
+constexpr int REORDER_MAX = 32;
+struct ReorderJob { const char* src; char* dst; size_t src_pitch, dst_pitch; int bytes, step; };   // step: 16, 8, 4, 2 or 1 bytes at a time
+struct ReorderJobs { ReorderJob job[REORDER_MAX]; };
+void launch_search_reorder(const ReorderJobs& jobs, int n, const int32_t* rows, int count, int src_rows, hipStream_t st);
+
+// ---- shared ------------------------------------------------------------------------------------------
+// An fp32 number as three bf16 that add up to it, cut off rather than rounded (8 + 8 + 8 bits; none can overflow).  Infinities and NaN
+// stand in the first part alone.
+struct Parts3 { uint32_t h, m, l; };                       // bits as of an fp32, lower half 0
+__device__ __forceinline__ Parts3 parts3(float x) {
+  const uint32_t u = __float_as_uint(x);
+  if ((u & 0x7f800000u) == 0x7f800000u) return {(u & 0x007fffffu) ? 0x7fc00000u : u, 0u, 0u};
+  Parts3 p;
+  p.h = u & 0xffff0000u;
+  const float r = x - __uint_as_float(p.h);
+  p.m = __float_as_uint(r) & 0xffff0000u;
+  p.l = __float_as_uint(r - __uint_as_float(p.m)) & 0xffff0000u;
+  return p;
+}
+__device__ __forceinline__ uint32_t pack_hi(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }   // upper halves of both
+
+// 8 consecutive elements of x from k on (k < K: as many as there are, then 0) as operand parts: 1 of bf16, 3 of fp32.
+template <typename T> constexpr int OPERAND_PARTS = sizeof(T) == 2 ? 1 : 3;
+__device__ __forceinline__ void load_operand(const bf16_t* p, int n, bool wide, Frag<bf16_t> (&f)[1]) {
+  if (n >= 8 && wide) { f[0].load(p); return; }
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+  f[0].v = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void split_operand(const float (&x)[8], Frag<bf16_t> (&f)[3]) {
+  uint32_t h[4], m[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const Parts3 a = parts3(x[2 * i]), b = parts3(x[2 * i + 1]);
+    h[i] = pack_hi(a.h, b.h); m[i] = pack_hi(a.m, b.m); l[i] = pack_hi(a.l, b.l);
+  }
+  f[0].v = make_uint4(h[0], h[1], h[2], h[3]);
+  f[1].v = make_uint4(m[0], m[1], m[2], m[3]);
+  f[2].v = make_uint4(l[0], l[1], l[2], l[3]);
+}
+__device__ __forceinline__ void load_operand(const float* p, int n, bool wide, Frag<bf16_t> (&f)[3]) {
+  float x[8];
+  if (n >= 8 && wide) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : 0.f;
+  }
+  split_operand(x, f);
+}
+
+}  // namespace cmt

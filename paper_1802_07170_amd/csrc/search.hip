@@ -1,0 +1,277 @@
+// A beam search's choice on logits that the caller has, and the rows that follow it.
+//
+// Extension v of hypothesis s scores c_s + z_sv - lse_s.  The logits are read once: a wavefront leaves the maximum and the sum of
+// exponentials of every 512 of them.  One workgroup per sentence then has each row's lse from those, finds the n groups whose best
+// extensions are best - they hold the n best extensions - and reads their entries again, n x 512.  Extensions are compared in 64
+// bits, equal ones by (slot, token): the first is better.  The first pass is bound by its read, the second by its chain of steps.
+#include <algorithm>
+
+#include "lowbit.h"
+
+namespace cmt {
+
+__device__ __forceinline__ unsigned search_sortable(float v) {   // larger numbers as larger unsigned ones
+  const unsigned u = __float_as_uint(v + 0.f);
+  return u ^ ((int)u < 0 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float search_wave_max(float v) {
+#define STEP(ctrl, rows) v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), ctrl, rows, 0xf, false)))
+  STEP(0x111, 0xf); STEP(0x112, 0xf); STEP(0x114, 0xf); STEP(0x118, 0xf);
+  STEP(0x142, 0xa);
+  STEP(0x143, 0xc);
+#undef STEP
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// ---- statistics of the groups ---------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void search_groups_kernel(const T* __restrict__ logits, size_t ld, const float* __restrict__ scores, int rows, int V,
+                                                            int groups, int wide, float2* __restrict__ stat) {
+  const int lane = threadIdx.x & 63;
+  const int id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = id / groups, g = id - row * groups;
+  if (row >= rows || !(scores[row] > -INFINITY)) return;     // (nothing reads a dead row's)
+  const T* p = logits + (size_t)row * ld;
+  const int v0 = g * SEARCH_GROUP;
+  float x[8];
+  if (wide && v0 + SEARCH_GROUP <= V) {
+    if (sizeof(T) == 2) {
+      Frag<T> f;
+      f.load(p + v0 + 8 * lane);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = f.get(i);
+    } else {
+      const float4 a = *reinterpret_cast<const float4*>((const float*)p + v0 + 4 * lane), b = *reinterpret_cast<const float4*>((const float*)p + v0 + 256 + 4 * lane);
+      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = v0 + 64 * i + lane < V ? to_f(p[v0 + 64 * i + lane]) : -INFINITY;
+  }
+  float mx = x[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[i]);          // (a NaN is never the largest, but is in the sum)
+  mx = search_wave_max(mx);
+  const float ms = mx > -INFINITY ? mx : 0.f;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum += expf(x[i] - ms);
+  sum = wave_sum(sum);
+  if (lane == 0) stat[id] = make_float2(mx, sum);
+}
+
+// ---- the choice --------------------------------------------------------------------------------------------
+constexpr int SELECT_NT = 1024, SELECT_NW = SELECT_NT / 64, SELECT_CAP = 1024;
+__device__ __forceinline__ bool better(double a, unsigned ia, double b, unsigned ib) { return a > b || (a == b && ia < ib); }
+
+struct SelectShared {
+  double base[SEARCH_MAX];
+  double lv[SELECT_CAP]; unsigned li[SELECT_CAP];            // a list of candidates
+  double wv[SEARCH_MAX]; unsigned wi[SEARCH_MAX];            // the best of them, in order
+  unsigned bound[SELECT_NW];
+  double rv[SELECT_NW]; unsigned ri[SELECT_NW];
+  int count;
+};
+// The n best of `total` items into sh.wv / sh.wi (returns how many there are).  value(i, index) gives an item's value (-inf: it does not
+// take part) and index.  least: items below it (as fp32) are known not to be among them.
+// Items that reach it are listed and each counts how many are better; a list that overflows - equal values in great number - is
+// answered by n rounds of a workgroup-wide maximum.
+template <typename F>
+__device__ __forceinline__ int select_best(SelectShared& sh, int n, int total, float least, F value) {
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  if (t == 0) sh.count = 0;
+  __syncthreads();
+  for (int i0 = 0; i0 < total; i0 += SELECT_NT) {
+    unsigned index = 0;
+    const double v = i0 + t < total ? value(i0 + t, index) : -INFINITY;
+    const bool take = v > -INFINITY && (float)v >= least;
+    const unsigned long long mask = __ballot(take);
+    if (!mask) continue;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&sh.count, __popcll(mask));
+    at = __builtin_amdgcn_readfirstlane(at) + __popcll(mask & ((1ull << lane) - 1));
+    if (take && at < SELECT_CAP) { sh.lv[at] = v; sh.li[at] = index; }
+  }
+  __syncthreads();
+  const int count = sh.count;
+  if (count <= SELECT_CAP) {
+    for (int i = t; i < count; i += SELECT_NT) {
+      const double v = sh.lv[i];
+      const unsigned ix = sh.li[i];
+      int place = 0;
+#pragma unroll 4
+      for (int k = 0; k < count; ++k) place += better(sh.lv[k], sh.li[k], v, ix);
+      if (place < n) { sh.wv[place] = v; sh.wi[place] = ix; }
+    }
+    __syncthreads();
+    return min(count, n);
+  }
+  double last = INFINITY;
+  unsigned last_index = 0;
+  for (int round = 0; round < n; ++round) {                  // (more than SELECT_CAP take part: there is a best one in each round)
+    double bv = -INFINITY;
+    unsigned bi = 0xffffffffu;
+#pragma unroll 1
+    for (int i = t; i < total; i += SELECT_NT) {
+      unsigned index = 0;
+      const double v = value(i, index);
+      if (v > -INFINITY && (round == 0 || better(last, last_index, v, index)) && better(v, index, bv, bi)) { bv = v; bi = index; }
+    }
+#pragma unroll 1
+    for (int o = 32; o > 0; o >>= 1) {
+      const double ov = __shfl_xor(bv, o, 64);
+      const unsigned oi = __shfl_xor(bi, o, 64);
+      if (better(ov, oi, bv, bi)) { bv = ov; bi = oi; }
+    }
+    if (lane == 0) { sh.rv[w] = bv; sh.ri[w] = bi; }
+    __syncthreads();
+    bv = sh.rv[0]; bi = sh.ri[0];
+#pragma unroll 1
+    for (int k = 1; k < SELECT_NW; ++k)
+      if (better(sh.rv[k], sh.ri[k], bv, bi)) { bv = sh.rv[k]; bi = sh.ri[k]; }
+    if (t == 0) { sh.wv[round] = bv; sh.wi[round] = bi; }
+    last = bv; last_index = bi;
+    __syncthreads();
+  }
+  return n;
+}
+template <typename T, bool ADVANCE>
+__global__ __launch_bounds__(SELECT_NT) void search_select_kernel(const T* __restrict__ logits, size_t ld, const float* __restrict__ scores,
+                                                                  const float2* __restrict__ stat, int K, int V, int groups, int n,
+                                                                  float* __restrict__ out_scores, int32_t* __restrict__ out_rows,
+                                                                  int32_t* __restrict__ out_tokens, SearchAdvance adv) {
+  __shared__ SelectShared sh;
+  __shared__ unsigned s_top[SEARCH_MAX];
+  const int b = blockIdx.x, t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), row0 = b * K;
+  for (int s = w; s < K; s += SELECT_NW) {                   // a row's score less its lse; -inf: it takes no part
+    const float c = scores[row0 + s];
+    double base = -INFINITY;
+    if (c > -INFINITY) {
+      const float2* p = stat + (size_t)(row0 + s) * groups;
+      float mx = -INFINITY;
+      for (int g = lane; g < groups; g += 64) mx = fmaxf(mx, p[g].x);
+      mx = search_wave_max(mx);
+      float sum = 0.f;
+      const float ms = mx > -INFINITY ? mx : 0.f;
+      for (int g = lane; g < groups; g += 64) { const float2 x = p[g]; sum += x.x > -INFINITY ? x.y * expf(x.x - ms) : x.y; }
+      sum = wave_sum(sum);
+      // (no finite logit, an infinite one or one that is no number: no extension of this row)
+      if (c < INFINITY && mx > -INFINITY && mx < INFINITY && sum < INFINITY) base = (double)c - (double)mx - (double)logf(sum);
+    }
+    if (lane == 0) sh.base[s] = base;
+  }
+  __syncthreads();
+  const int total = K * groups;
+  auto group = [&](int i, unsigned& index) {
+    const int s = i / groups;
+    index = i;
+    const double base = sh.base[s];
+    return base > -INFINITY ? base + (double)stat[(size_t)row0 * groups + i].x : -(double)INFINITY;
+  };
+  // the n-th best of a wavefront's lanes' best is a bound that n groups reach
+  float tv = -INFINITY;
+  for (int i = t; i < total; i += SELECT_NT) { unsigned ix; tv = fmaxf(tv, (float)group(i, ix)); }
+  const unsigned key = search_sortable(tv);
+  unsigned least = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 0; --bit)
+    if (__popcll(__ballot(key >= (least | 1u << bit))) >= n) least |= 1u << bit;
+  if (lane == 0) sh.bound[w] = least;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < SELECT_NW; ++i) least = max(least, sh.bound[i]);
+  const float bound = least < 0x00800000u ? -INFINITY : __uint_as_float((int)least < 0 ? least ^ 0x80000000u : ~least);
+  const int tops = select_best(sh, n, total, bound, group);
+  if (t < tops) s_top[t] = sh.wi[t];
+  const float floor_ = tops == n ? (float)sh.wv[n - 1] : -INFINITY;
+  __syncthreads();
+  const int found = select_best(sh, n, tops * SEARCH_GROUP, floor_, [&](int i, unsigned& index) {
+    const int id = s_top[i / SEARCH_GROUP], s = id / groups, v = (id - s * groups) * SEARCH_GROUP + i % SEARCH_GROUP;
+    index = (unsigned)s * (unsigned)V + (unsigned)v;
+    if (v >= V) return -(double)INFINITY;
+    const float z = to_f(logits[(size_t)(row0 + s) * ld + v]);
+    return z > -INFINITY ? sh.base[s] + (double)z : -(double)INFINITY;
+  });
+  if (!ADVANCE) {
+    if (t < n) {
+      const bool in = t < found;
+      const unsigned ix = in ? sh.wi[t] : 0, s = ix / (unsigned)V;
+      out_scores[(size_t)b * n + t] = in ? (float)sh.wv[t] : -INFINITY;
+      out_rows[(size_t)b * n + t] = in ? row0 + (int)s : -1;
+      out_tokens[(size_t)b * n + t] = in ? (int)(ix - s * (unsigned)V) : -1;
+    }
+    return;
+  }
+  // ---- a search kept on the device: n = K, the winners split into finished and live hypotheses ------------------
+  if (t >= 64) return;
+  const bool won = t < found;
+  const double v = won ? sh.wv[t] : -INFINITY;
+  const unsigned ix = won ? sh.wi[t] : 0;
+  const int s = ix / (unsigned)V, tk = ix - (unsigned)s * (unsigned)V;
+  const bool fin = won && (tk == adv.eos || adv.j == adv.max_len - 1), live = won && !fin;
+  const unsigned long long m_fin = __ballot(fin), m_live = __ballot(live);
+  const int n_new = __popcll(m_live);
+  if (live) {
+    const int r = row0 + __popcll(m_live & ((1ull << t) - 1));
+    out_scores[r] = (float)v;
+    out_rows[r] = row0 + s;
+    out_tokens[r] = tk;
+    adv.hist_tok[(size_t)adv.j * adv.hist_ld + r] = tk;
+    adv.hist_par[(size_t)adv.j * adv.hist_ld + r] = s;
+  }
+  if (t >= n_new && t < K) { out_scores[row0 + t] = -INFINITY; out_rows[row0 + t] = -1; out_tokens[row0 + t] = -1; }
+  if (m_fin) {
+    const float norm = (float)v / powf((5.f + (float)(adv.j + 1)) / 6.f, adv.alpha);
+    float best = adv.fin_score[b];
+    int at = -1;
+    for (unsigned long long m = m_fin; m; m &= m - 1) {
+      const int q = __ffsll(m) - 1;
+      const float x = __shfl(norm, q, 64);
+      if (x > best) { best = x; at = q; }                    // strict: the hypothesis finished first keeps a tie
+    }
+    if (t == at) { adv.fin_score[b] = best; adv.fin_step[b] = adv.j; adv.fin_par[b] = s; adv.fin_tok[b] = tk; }
+  }
+}
+static int search_groups(int V) { return (V + SEARCH_GROUP - 1) / SEARCH_GROUP; }
+size_t search_workspace(int B, int K, int V) { return (size_t)B * K * search_groups(V) * sizeof(float2); }
+void launch_search_select(int prec, const void* logits, size_t ld, const float* scores, int B, int K, int V, int n, float* out_scores,
+                          int32_t* out_rows, int32_t* out_tokens, const SearchAdvance* adv, void* workspace, hipStream_t st) {
+  const int groups = search_groups(V);
+  const int wide = (((uintptr_t)logits | ld * (prec ? 2 : 4)) & 15) == 0;
+  float2* stat = (float2*)workspace;
+  const dim3 grid((unsigned)(((long)B * K * groups + 3) / 4));
+  auto go = [&](auto type) {
+    using T = decltype(type);
+    hipLaunchKernelGGL(search_groups_kernel<T>, grid, dim3(256), 0, st, (const T*)logits, ld, scores, B * K, V, groups, wide, stat);
+    if (adv)
+      hipLaunchKernelGGL((search_select_kernel<T, true>), dim3(B), dim3(SELECT_NT), 0, st, (const T*)logits, ld, scores, stat, K, V, groups, n, out_scores,
+                         out_rows, out_tokens, *adv);
+    else
+      hipLaunchKernelGGL((search_select_kernel<T, false>), dim3(B), dim3(SELECT_NT), 0, st, (const T*)logits, ld, scores, stat, K, V, groups, n, out_scores,
+                         out_rows, out_tokens, SearchAdvance{});
+  };
+  if (prec) go(bf16_t{}); else go(float{});
+}
+
+// ---- rows that follow ----------------------------------------------------------------------------------------
+// dst[r] = src[rows[r]] of several tensors; rows whose number is outside the source stay as they were
+template <typename V>
+__device__ __forceinline__ void reorder_row(const char* s, char* d, int bytes) {
+  for (int i = threadIdx.x; i < bytes / (int)sizeof(V); i += 128) reinterpret_cast<V*>(d)[i] = reinterpret_cast<const V*>(s)[i];
+}
+__global__ __launch_bounds__(128) void search_reorder_kernel(ReorderJobs jobs, const int32_t* __restrict__ rows, int src_rows) {
+  const int r = blockIdx.x, from = rows[r];
+  if ((unsigned)from >= (unsigned)src_rows) return;
+  const ReorderJob& j = jobs.job[blockIdx.y];
+  const char* s = j.src + (size_t)from * j.src_pitch;
+  char* d = j.dst + (size_t)r * j.dst_pitch;
+  if (j.step == 16) reorder_row<uint4>(s, d, j.bytes);
+  else if (j.step == 4) reorder_row<uint32_t>(s, d, j.bytes);
+  else if (j.step == 2) reorder_row<uint16_t>(s, d, j.bytes);
+  else reorder_row<uint8_t>(s, d, j.bytes);
+}
+void launch_search_reorder(const ReorderJobs& jobs, int n, const int32_t* rows, int count, int src_rows, hipStream_t st) {
+  hipLaunchKernelGGL(search_reorder_kernel, dim3(count, n), dim3(128), 0, st, jobs, rows, src_rows);
+}
+
+}  // namespace cmt

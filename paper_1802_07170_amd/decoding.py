@@ -1,0 +1,285 @@
+"""Decoding in small numbers, on torch tensors: products with 4-bit weights, attention over source rows held in 8 bits, and a
+beam search's choice with the states that follow it.  What the functions compute is defined in include/cytonmt_hip.h; this module checks
+its arguments, makes the tensors that are returned, and calls the library.
+
+Calls are enqueued on torch's current stream of the tensors' device and may be captured into a graph.  Nothing here is differentiable:
+a tensor that wants a gradient is refused.  There is no CPU fallback."""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import binding
+from .binding import CMT_OK, CmtCacheConfig, CmtCacheRows, CmtError, CmtReorderTensor
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _check(rc):
+    if rc != CMT_OK:
+        raise CmtError(rc, binding.load_library().cmt_operator_error().decode())
+
+
+def _tensor(t, name, dims, dtypes, device=None):
+    """Refuses what the kernels do not take: the last dimension's elements lie side by side, the other strides are free."""
+    if not isinstance(t, torch.Tensor) or t.dim() not in dims:
+        raise ValueError(f"{name} must be a tensor of {' or '.join(map(str, dims))} dimensions")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be of {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a GPU, not on {t.device}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name}: the elements of the last dimension must lie side by side")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} wants a gradient: these operators have none (use torch.no_grad())")
+
+
+def _pitch(t):
+    """Elements from one row of a matrix to the next."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class _On:
+    """The device of the tensors as the current one, and its current stream."""
+
+    def __init__(self, device):
+        self.device, self.other = device, None
+
+    def __enter__(self):
+        if self.device.index != torch.cuda.current_device():
+            self.other = torch.cuda.device(self.device)
+            self.other.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *error):
+        if self.other is not None:
+            self.other.__exit__(*error)
+
+
+class QuantWeight:
+    """A weight [outputs, inputs] in 4 bits, with a bf16 scale for every `group` (32, 64 or 128) inputs of a row."""
+
+    def __init__(self, outputs, inputs, group, device):
+        size = C.c_size_t()
+        _check(binding.load_library().cmt_quant_weight_bytes(outputs, inputs, group, C.byref(size)))
+        self.outputs, self.inputs, self.group = outputs, inputs, group
+        self.packed = torch.empty(size.value, dtype=torch.uint8, device=device)
+
+    @property
+    def device(self):
+        return self.packed.device
+
+    @classmethod
+    def pack(cls, weight, group=64):
+        """From a weight [outputs, inputs] in fp32 or bf16: scale = bf16(max|w| / 6) and the nearest codes."""
+        _tensor(weight, "weight", (2,), _TYPES)
+        w = cls(*weight.shape, group, weight.device)
+        with _On(w.device) as stream:
+            _check(binding.load_library().cmt_quant_weight_pack(weight.data_ptr(), _TYPES[weight.dtype], _pitch(weight), w.outputs, w.inputs, group,
+                                                                w.packed.data_ptr(), stream))
+        return w
+
+    @classmethod
+    def from_codes(cls, codes, scales, group):
+        """From e2m1 codes [outputs, inputs] (uint8, one to a byte) and bf16 scales [outputs, ceil(inputs / group)]."""
+        _tensor(codes, "codes", (2,), (torch.uint8,))
+        _tensor(scales, "scales", (2,), (torch.bfloat16,), codes.device)
+        w = cls(*codes.shape, group, codes.device)
+        if tuple(scales.shape) != (w.outputs, -(-w.inputs // group)):
+            raise ValueError(f"scales must be {(w.outputs, -(-w.inputs // group))}, not {tuple(scales.shape)}")
+        if not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError("codes and scales must be contiguous")
+        with _On(w.device) as stream:
+            _check(binding.load_library().cmt_quant_weight_encode(codes.data_ptr(), scales.data_ptr(), w.outputs, w.inputs, group, w.packed.data_ptr(),
+                                                                  stream))
+        return w
+
+    def values(self):
+        """The weight that the codes stand for, fp32 [outputs, inputs]."""
+        out = torch.empty(self.outputs, self.inputs, dtype=torch.float32, device=self.device)
+        with _On(self.device) as stream:
+            _check(binding.load_library().cmt_quant_weight_values(self.packed.data_ptr(), self.outputs, self.inputs, self.group, out.data_ptr(), stream))
+        return out
+
+
+def quant_product(x, weight, bias=None, tanh=False, out_dtype=None, out=None):
+    """x [rows, inputs] (fp32 or bf16) times the 4-bit weight's transpose, plus an fp32 bias [outputs], through tanh if asked for:
+    [rows, outputs] in `out_dtype` (x's type if None), or in `out`."""
+    _tensor(x, "x", (2,), _TYPES, weight.device)
+    rows = x.shape[0]
+    if x.shape[1] != weight.inputs:
+        raise ValueError(f"x has {x.shape[1]} columns, the weight {weight.inputs} inputs")
+    if bias is not None:
+        _tensor(bias, "bias", (1,), (torch.float32,), x.device)
+        if bias.shape[0] != weight.outputs:
+            raise ValueError(f"bias has {bias.shape[0]} elements, the weight {weight.outputs} outputs")
+    if out is None:
+        dtype = x.dtype if out_dtype is None else out_dtype
+        if dtype not in _TYPES:
+            raise ValueError(f"out_dtype must be torch.float32 or torch.bfloat16, not {dtype}")
+        out = torch.empty((rows, weight.outputs), dtype=dtype, device=x.device)
+    else:
+        _tensor(out, "out", (2,), _TYPES if out_dtype is None else (out_dtype,), x.device)
+        if tuple(out.shape) != (rows, weight.outputs):
+            raise ValueError(f"out must be {(rows, weight.outputs)}, not {tuple(out.shape)}")
+        _apart(out, "out", x, "x")
+    with _On(x.device) as stream:
+        _check(binding.load_library().cmt_quant_product(
+            x.data_ptr(), _TYPES[x.dtype], _pitch(x), rows, weight.packed.data_ptr(), weight.outputs, weight.inputs, weight.group,
+            None if bias is None else bias.data_ptr(), bool(tanh), out.data_ptr(), _TYPES[out.dtype], _pitch(out), stream))
+    return out
+
+
+def _apart(a, name, b, other):
+    """Refuses two tensors of rows (first dimension; the others side by side) that share memory.  Columns of one matrix may lie beside each other."""
+    (a0, ap, an, al), (b0, bp, bn, bl) = ((t.data_ptr(), t.stride(0) * t.element_size(), t.shape[0], t[0].numel() * t.element_size() if len(t) else 0)
+                                          for t in (a, b))
+    if not (an and bn and al and bl) or a0 >= b0 + (bn - 1) * bp + bl or b0 >= a0 + (an - 1) * ap + al:
+        return
+    ahead = (b0 - a0) % ap if ap > 0 else 0
+    if ap != bp or an == 1 or bn == 1 or ahead < al or ahead + bl > ap:
+        raise ValueError(f"{name} overlaps {other}")
+
+
+class SourceCache:
+    """Keys and values of up to `max_tokens` tokens of each sequence in 8 bits, a scale for every 32 tokens and head."""
+
+    def __init__(self, sequences, heads, head_dim, max_tokens, device="cuda"):
+        self.config = CmtCacheConfig(sequences, heads, head_dim, max_tokens)
+        size = C.c_size_t()
+        _check(binding.load_library().cmt_cache_bytes(C.byref(self.config), C.byref(size)))
+        self.sequences, self.heads, self.head_dim, self.max_tokens = sequences, heads, head_dim, max_tokens
+        self.data = torch.empty(size.value, dtype=torch.uint8, device=device)
+        self.tokens = 0                                    # bound of the lengths, from the last fill
+        self._needs = {}                                   # bytes of workspace by (tokens, rows per sequence, query heads)
+
+    @property
+    def device(self):
+        return self.data.device
+
+    def fill(self, keys, values, lengths):
+        """Writes tokens [0, lengths[s]) of every sequence: keys, values [sequences, tokens, heads, head_dim] in fp32 or bf16, lengths int32
+        [sequences] on the device (clamped to [0, tokens])."""
+        _tensor(keys, "keys", (4,), _TYPES, self.device)
+        _tensor(values, "values", (4,), (keys.dtype,), self.device)
+        _tensor(lengths, "lengths", (1,), (torch.int32,), self.device)
+        want = (self.sequences, keys.shape[1], self.heads, self.head_dim)
+        if tuple(keys.shape) != want or tuple(values.shape) != want or not 1 <= want[1] <= self.max_tokens:
+            raise ValueError(f"keys and values must be ({self.sequences}, 1..{self.max_tokens}, {self.heads}, {self.head_dim}), not "
+                             f"{tuple(keys.shape)} and {tuple(values.shape)}")
+        if lengths.shape[0] != self.sequences:
+            raise ValueError(f"lengths must have {self.sequences} elements, not {lengths.shape[0]}")
+        rows = [CmtCacheRows(t.data_ptr(), *t.stride()[:3]) for t in (keys, values)]
+        with _On(self.device) as stream:
+            _check(binding.load_library().cmt_cache_fill(C.byref(self.config), self.data.data_ptr(), C.byref(rows[0]), C.byref(rows[1]),
+                                                         _TYPES[keys.dtype], lengths.data_ptr(), want[1], stream))
+        self.tokens = want[1]
+        return self
+
+    def read(self):
+        """The keys and values that the cache stands for: fp32 [sequences, tokens of the last fill, heads, head_dim], 0 behind a length."""
+        self._filled()
+        keys = torch.empty(self.sequences, self.tokens, self.heads, self.head_dim, dtype=torch.float32, device=self.device)
+        values = torch.empty_like(keys)
+        with _On(self.device) as stream:
+            _check(binding.load_library().cmt_cache_read(C.byref(self.config), self.data.data_ptr(), self.tokens, keys.data_ptr(), values.data_ptr(),
+                                                         stream))
+        return keys, values
+
+    def attend(self, query, scale=1.0, out=None):
+        """Attention of query [rows, query heads, head_dim] (fp32 or bf16): rows a multiple of the sequences, row r belonging to sequence
+        r // (rows / sequences); query heads a multiple of the heads, in order.  Returns the same shape and type (0 for a sequence of
+        length 0)."""
+        self._filled()
+        _tensor(query, "query", (3,), _TYPES, self.device)
+        rows, heads, dim = query.shape
+        if rows == 0 or rows % self.sequences or heads == 0 or heads % self.heads or dim != self.head_dim:
+            raise ValueError(f"query must be (a multiple of {self.sequences}, a multiple of {self.heads}, {self.head_dim}), not {tuple(query.shape)}")
+        if out is None:
+            out = torch.empty((rows, heads, dim), dtype=query.dtype, device=self.device)
+        else:
+            _tensor(out, "out", (3,), (query.dtype,), self.device)
+            if out.shape != query.shape:
+                raise ValueError(f"out must be {tuple(query.shape)}, not {tuple(out.shape)}")
+            _apart(out, "out", query, "query")
+        for t, name in ((query, "query"), (out, "out")):
+            if heads > 1 and t.stride(1) != dim:
+                raise ValueError(f"{name}: the heads of a row must lie side by side")
+        lib, per = binding.load_library(), rows // self.sequences
+        key = (self.tokens, per, heads)
+        need = self._needs.get(key)
+        if need is None:
+            size = C.c_size_t()
+            _check(lib.cmt_cache_attend_workspace(C.byref(self.config), per, heads, self.tokens, C.byref(size)))
+            need = self._needs[key] = size.value
+        with _On(self.device) as stream:
+            work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+            _check(lib.cmt_cache_attend(
+                C.byref(self.config), self.data.data_ptr(), query.data_ptr(), _TYPES[query.dtype], query.stride(0) if rows > 1 else heads * dim, per,
+                heads, self.tokens, scale, out.data_ptr(), out.stride(0) if rows > 1 else heads * dim, None if work is None else work.data_ptr(), need,
+                stream))
+        return out
+
+    def _filled(self):
+        if not self.tokens:
+            raise ValueError("the cache has not been filled")
+
+
+def beam_select(logits, scores, n=None):
+    """The n (the beam if None) best one-token extensions of each sentence's hypotheses: logits [sentences * beam, vocab] (fp32 or bf16), scores
+    fp32 [sentences, beam], -inf for a place without a hypothesis.  Returns scores fp32, rows int32 (b * beam + s, the
+    hypothesis that is extended) and tokens int32, [sentences, n] each: best first, of equal ones the lower (row, token), and -inf, -1, -1 where
+    there are fewer."""
+    _tensor(logits, "logits", (2,), _TYPES)
+    _tensor(scores, "scores", (2,), (torch.float32,), logits.device)
+    sentences, beam = scores.shape
+    if logits.shape[0] != sentences * beam:
+        raise ValueError(f"logits have {logits.shape[0]} rows, scores {sentences} x {beam} places")
+    if not scores.is_contiguous():
+        raise ValueError("scores must be contiguous")
+    n, lib, vocab = beam if n is None else n, binding.load_library(), logits.shape[1]
+    size = C.c_size_t()
+    _check(lib.cmt_beam_select_workspace(sentences, beam, vocab, C.byref(size)))
+    with _On(logits.device) as stream:
+        new = torch.empty((sentences, n), dtype=torch.float32, device=logits.device)
+        rows, tokens = torch.empty((2, sentences, n), dtype=torch.int32, device=logits.device).unbind(0)
+        work = torch.empty(size.value, dtype=torch.uint8, device=logits.device)
+        _check(lib.cmt_beam_select(logits.data_ptr(), _TYPES[logits.dtype], _pitch(logits), scores.data_ptr(), sentences, beam, vocab, n,
+                                   new.data_ptr(), rows.data_ptr(), tokens.data_ptr(), work.data_ptr(), size.value, stream))
+    return new, rows, tokens
+
+
+def beam_reorder(rows, sources, targets):
+    """targets[i][r] = sources[i][rows[r]] for all tensors in one launch per 32: rows int32 of any shape (as beam_select returns them), the
+    tensors' first dimension counting rows, the others contiguous.  Target rows whose number is outside the source stay as they were."""
+    if not isinstance(rows, torch.Tensor) or rows.dtype != torch.int32 or not rows.is_contiguous() or not rows.is_cuda:
+        raise ValueError("rows must be a contiguous int32 tensor on a GPU")
+    if len(sources) != len(targets):
+        raise ValueError(f"{len(sources)} sources and {len(targets)} targets")
+    count, source_rows = rows.numel(), sources[0].shape[0] if sources else 0
+    jobs = (CmtReorderTensor * len(sources))()
+    for i, (a, b) in enumerate(zip(sources, targets)):
+        if a.dtype != b.dtype or a.device != rows.device or b.device != rows.device:
+            raise ValueError(f"tensors {i} must be of one type and on the device of rows")
+        if a.dim() == 0 or a.shape[1:] != b.shape[1:] or a.shape[0] != source_rows or b.shape[0] != count:
+            raise ValueError(f"tensors {i} must have {source_rows} and {count} rows alike, not {tuple(a.shape)} and {tuple(b.shape)}")
+        if (a.requires_grad or b.requires_grad) and torch.is_grad_enabled():
+            raise ValueError(f"tensors {i} want a gradient: these operators have none (use torch.no_grad())")
+        size, width = a.element_size(), 1
+        for t in (a, b):
+            width = 1
+            for d in range(t.dim() - 1, 0, -1):
+                if t.shape[d] > 1 and t.stride(d) != width:
+                    raise ValueError(f"tensors {i}: the elements of a row must lie side by side")
+                width *= t.shape[d]
+        job = jobs[i]
+        job.source, job.target, job.row_bytes = a.data_ptr(), b.data_ptr(), width * size
+        job.source_pitch = (a.stride(0) if a.shape[0] > 1 else width) * size
+        job.target_pitch = (b.stride(0) if b.shape[0] > 1 else width) * size
+    if not sources or not count or not source_rows:
+        return
+    with _On(rows.device) as stream:
+        _check(binding.load_library().cmt_beam_reorder(rows.data_ptr(), count, source_rows, jobs, len(sources), stream))
