@@ -105,7 +105,7 @@ def load_library():
     lib.cmt_cache_attend.argtypes = [cachep, vp, vp, i32, i64, i32, i32, i32, C.c_float, vp, i64, vp, sz, vp]
     lib.cmt_beam_select_workspace.argtypes = [i32, i32, i32, szp]
     lib.cmt_beam_select.argtypes = [vp, i32, i64, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
-    lib.cmt_beam_reorder.argtypes = [vp, i32, i32, C.POINTER(CmtReorderTensor), i32, vp]
+    lib.cmt_beam_reorder.argtypes = [vp, i32, i32, vp, i32, vp]            # (an array of CmtReorderTensor)
     for name in EXPORTS:
         if name not in ("cmt_destroy", "cmt_last_error", "cmt_operator_error"):
             getattr(lib, name).restype = C.c_int

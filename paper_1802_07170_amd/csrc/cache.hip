@@ -37,12 +37,13 @@ __device__ __forceinline__ void fill_load(const T* p, int n, bool wide, float (&
     for (int i = 0; i < 16; ++i) x[i] = i < n ? to_f(p[i]) : 0.f;
   }
 }
-// One workgroup per block of 32 tokens, sequence and head; blockIdx.z: keys, values.
-template <typename T>
-__global__ __launch_bounds__(256) void cache_fill_kernel(CacheSource src, const int32_t* __restrict__ lengths, int tokens, CacheShape s, CacheView c, int wide) {
-  __shared__ __align__(16) int8_t code[CACHE_BLOCK * (1024 + FILL_PAD)];
-  __shared__ float s_most[4];
-  __shared__ int s_bad[4];
+// One workgroup per block of 32 tokens, sequence and head; blockIdx.z: keys, values.  The block is read once: a thread keeps its NS
+// slots of 16 d of a token until the scale is known.
+template <typename T, int NS>
+__global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const int32_t* __restrict__ lengths, int tokens, CacheShape s, CacheView c, int wide) {
+  __shared__ __align__(16) int8_t code[CACHE_BLOCK * (256 * NS + FILL_PAD)];
+  __shared__ float s_most[8];
+  __shared__ int s_bad[8];
   const int b = blockIdx.y / s.heads, head = blockIdx.y % s.heads, blk = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
   const bool is_v = blockIdx.z;
   const int len = min(max(lengths[b], 0), tokens);
@@ -52,50 +53,60 @@ __global__ __launch_bounds__(256) void cache_fill_kernel(CacheSource src, const 
   const size_t tok = is_v ? src.v_tok : src.k_tok;
   const T* p = (const T*)(is_v ? src.v : src.k) + (size_t)b * (is_v ? src.v_seq : src.k_seq) + (size_t)head * (is_v ? src.v_head : src.k_head) +
                (size_t)blk * CACHE_BLOCK * tok;
-  const int chunks = s.chunks(), ld = chunks * 64 + FILL_PAD, slots = chunks * 128;   // a slot: 16 d of a token
+  const int chunks = s.chunks(), ld = chunks * 64 + FILL_PAD, slots = chunks * 128;   // at most 512 NS
   const bool wd = wide >> is_v & 1;
-  float x[16], most = 0.f;
+  float x[NS][16], most = 0.f;
   bool bad = false;
-  for (int i = t; i < slots; i += 256) {
-    const int r = (i & 15) + 16 * (i >> 6 & 1), d = 64 * (i >> 7) + 16 * (i >> 4 & 3);
-    if (r >= n || d >= s.dim) continue;
-    fill_load(p + (size_t)r * tok + d, s.dim - d, wd, x);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) { most = fmaxf(most, fabsf(x[e])); bad |= !(fabsf(x[e]) <= 3.4028235e38f); }
+  for (int k = 0; k < NS; ++k) {
+    const int i = k * 512 + t, r = (i & 15) + 16 * (i >> 6 & 1), d = 64 * (i >> 7) + 16 * (i >> 4 & 3);
+    fill_load(p + (size_t)r * tok + d, i < slots && r < n ? s.dim - d : 0, wd, x[k]);
   }
+#pragma unroll
+  for (int k = 0; k < NS; ++k)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) { most = fmaxf(most, fabsf(x[k][e])); bad |= !(fabsf(x[k][e]) <= 3.4028235e38f); }
   most = wave_max(most);
   const bool any = __ballot(bad) != 0;
   if (lane == 0) { s_most[w] = most; s_bad[w] = any; }
   __syncthreads();
-  most = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
-  const bool finite = !(s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3]);
+  bool finite = true;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) { most = fmaxf(most, s_most[k]); finite &= !s_bad[k]; }
   const float scale = finite ? most / 127.0f : __uint_as_float(0x7fc00000u);   // (a block with a number that is none: no result hides it)
   const size_t at = ((size_t)b * s.heads + head) * s.blocks() + blk;
   if (t == 0) (is_v ? c.vscale : c.kscale)[at] = scale;
   const bool some = scale > 0.f, tiny = scale < 1e-36f;
   const float inv = 1.0f / scale;
-  for (int i = t; i < slots; i += 256) {
-    const int r = (i & 15) + 16 * (i >> 6 & 1), d = 64 * (i >> 7) + 16 * (i >> 4 & 3);
-    uint32_t o[4] = {0, 0, 0, 0};
-    if (some && r < n && d < s.dim) {
-      fill_load(p + (size_t)r * tok + d, s.dim - d, wd, x);
 #pragma unroll
+  for (int k = 0; k < NS; ++k) {
+    const int i = k * 512 + t, r = (i & 15) + 16 * (i >> 6 & 1), d = 64 * (i >> 7) + 16 * (i >> 4 & 3);
+    uint32_t o[4] = {0, 0, 0, 0};
+    if (tiny && some) {                                      // (uniform; 1 / scale may be infinite)
+#pragma unroll 1
       for (int e = 0; e < 16; ++e) {
-        const int q = tiny ? (int)fmin(fmax(rint((double)x[e] / (double)scale), -127.0), 127.0) : (int)cache_code(x[e], scale, inv);
-        o[e >> 2] |= (uint32_t)(q & 255) << (8 * (e & 3));
+        float y = 0.f;
+#pragma unroll
+        for (int f = 0; f < 16; ++f) y = f == e ? x[k][f] : y;
+        const uint32_t q = (uint32_t)((int)fmin(fmax(rint((double)y / (double)scale), -127.0), 127.0) & 255) << (8 * (e & 3));
+#pragma unroll
+        for (int f = 0; f < 4; ++f) o[f] |= f == e >> 2 ? q : 0u;
       }
+    } else if (some) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[e >> 2] |= (uint32_t)((int)cache_code(x[k][e], scale, inv) & 255) << (8 * (e & 3));
     }
-    *reinterpret_cast<uint4*>(code + r * ld + d) = make_uint4(o[0], o[1], o[2], o[3]);
+    if (i < slots) *reinterpret_cast<uint4*>(code + r * ld + d) = make_uint4(o[0], o[1], o[2], o[3]);
   }
   __syncthreads();
   char* out = (is_v ? c.v : c.k) + at * chunks * 2048;
   if (!is_v) {
-    for (int i = t; i < slots; i += 256) {                   // [16-token tile][chunk][lane]
+    for (int i = t; i < slots; i += 512) {                   // [16-token tile][chunk][lane]
       const int tile = i / (chunks * 64), rest = i - tile * chunks * 64, ch = rest >> 6, l = rest & 63;
       *reinterpret_cast<uint4*>(out + (size_t)i * 16) = *reinterpret_cast<const uint4*>(code + (16 * tile + (l & 15)) * ld + 64 * ch + 16 * (l >> 4));
     }
   } else {
-    for (int i = t; i < slots; i += 256) {                   // [32 d][lane]
+    for (int i = t; i < slots; i += 512) {                   // [32 d][lane]
       const int l = i & 63, d = 32 * (i >> 6) + (l & 15), r = 4 * (l >> 4);
       uint32_t o[4];
 #pragma unroll
@@ -111,35 +122,57 @@ void launch_cache_fill(int prec, const CacheSource& src, const int32_t* lengths,
   const size_t es = prec ? 2 : 4;
   auto wide = [&](const void* p, size_t a, size_t b, size_t c) { return (((uintptr_t)p | a * es | b * es | c * es) & 15) == 0; };
   const int flags = (wide(src.k, src.k_seq, src.k_tok, src.k_head) ? 1 : 0) | (wide(src.v, src.v_seq, src.v_tok, src.v_head) ? 2 : 0);
-  const dim3 grid((unsigned)std::max(1, (tokens + CACHE_BLOCK - 1) / CACHE_BLOCK), (unsigned)(s.seqs * s.heads), 2);
-  if (prec) hipLaunchKernelGGL(cache_fill_kernel<bf16_t>, grid, dim3(256), 0, st, src, lengths, tokens, s, CacheView(s, cache), flags);
-  else hipLaunchKernelGGL(cache_fill_kernel<float>, grid, dim3(256), 0, st, src, lengths, tokens, s, CacheView(s, cache), flags);
+  const dim3 grid((unsigned)((tokens + CACHE_BLOCK - 1) / CACHE_BLOCK), (unsigned)(s.seqs * s.heads), 2);
+  auto go = [&](auto type, auto ns) {
+    hipLaunchKernelGGL((cache_fill_kernel<decltype(type), decltype(ns)::value>), grid, dim3(512), 0, st, src, lengths, tokens, s, CacheView(s, cache), flags);
+  };
+  auto by_width = [&](auto type) {
+    if (s.chunks() <= 4) go(type, std::integral_constant<int, 1>());
+    else if (s.chunks() <= 8) go(type, std::integral_constant<int, 2>());
+    else go(type, std::integral_constant<int, 4>());
+  };
+  if (prec) by_width(bf16_t{}); else by_width(float{});
 }
 
 // ---- reading back: [seqs, tokens, heads, dim], 0 behind a sequence's end -------------------------------------
-__global__ __launch_bounds__(256) void cache_read_kernel(CacheShape s, CacheView c, int tokens, float* __restrict__ k, float* __restrict__ v) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, n = (size_t)s.seqs * tokens * s.heads * s.dim;
-  if (i >= n) return;
-  float* const out = blockIdx.y ? v : k;
-  const int d = (int)(i % s.dim);
-  size_t r = i / s.dim;
-  const int head = (int)(r % s.heads);
-  r /= s.heads;
-  const int t = (int)(r % tokens), b = (int)(r / tokens);
-  float x = 0.f;
-  if (t < c.lengths[b]) {
-    const size_t at = ((size_t)b * s.heads + head) * s.blocks() + (t >> 5);
-    const char* base = (blockIdx.y ? c.v : c.k) + at * s.chunks() * 2048;
-    const int q = t & 15, hi = t >> 4 & 1;
-    const size_t off = blockIdx.y ? (size_t)(d >> 5) * 1024 + ((q >> 2) * 16 + (d & 15)) * 16 + 8 * (d >> 4 & 1) + 4 * hi + (q & 3)
-                                  : ((size_t)hi * s.chunks() + (d >> 6)) * 1024 + ((d >> 4 & 3) * 16 + q) * 16 + (d & 15);
-    x = (float)(int8_t)base[off] * (blockIdx.y ? c.vscale : c.kscale)[at];
+// One workgroup per block, sequence and head; blockIdx.z: keys, values.  The block's codes pass through LDS as they are.
+__global__ __launch_bounds__(256) void cache_read_kernel(CacheShape s, CacheView c, int tokens, int wide, float* __restrict__ k, float* __restrict__ v) {
+  __shared__ uint4 code[2048];
+  const int b = blockIdx.y / s.heads, head = blockIdx.y % s.heads, blk = blockIdx.x, t = threadIdx.x;
+  const bool is_v = blockIdx.z;
+  const int chunks = s.chunks(), t0 = blk * CACHE_BLOCK;
+  const int n = min(tokens - t0, CACHE_BLOCK), valid = min(c.lengths[b] - t0, n);
+  const size_t at = ((size_t)b * s.heads + head) * s.blocks() + blk;
+  float scale = 0.f;
+  if (valid > 0) {
+    const uint4* p = reinterpret_cast<const uint4*>((is_v ? c.v : c.k) + at * chunks * 2048);
+    for (int i = t; i < chunks * 128; i += 256) code[i] = p[i];
+    scale = (is_v ? c.vscale : c.kscale)[at];
   }
-  out[i] = x;
+  __syncthreads();
+  const int8_t* q = reinterpret_cast<const int8_t*>(code);
+  float* const out = (is_v ? v : k) + (((size_t)b * tokens + t0) * s.heads + head) * s.dim;
+  const size_t row = (size_t)s.heads * s.dim;
+  const int quads = (s.dim + 3) / 4;
+  for (int i = t; i < n * quads; i += 256) {
+    const int r = i / quads, d = (i - r * quads) * 4, lo = r & 15, hi = r >> 4;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    if (r < valid) {
+      const int8_t* o = q + (is_v ? (d >> 5) * 1024 + ((lo >> 2) * 16 + (d & 15)) * 16 + 8 * (d >> 4 & 1) + 4 * hi + (lo & 3)
+                                  : (hi * chunks + (d >> 6)) * 1024 + ((d >> 4 & 3) * 16 + lo) * 16 + (d & 15));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (float)o[is_v ? 16 * e : e] * scale;
+    }
+    float* const to = out + r * row + d;
+    if (wide) *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+    else
+      for (int e = 0; e < 4; ++e) if (d + e < s.dim) to[e] = x[e];
+  }
 }
 void launch_cache_read(const CacheShape& s, const void* cache, int tokens, float* k, float* v, hipStream_t st) {
-  const size_t n = (size_t)s.seqs * tokens * s.heads * s.dim;
-  hipLaunchKernelGGL(cache_read_kernel, dim3((unsigned)((n + 255) / 256), 2), dim3(256), 0, st, s, CacheView(s, const_cast<void*>(cache)), tokens, k, v);
+  const dim3 grid((unsigned)((tokens + CACHE_BLOCK - 1) / CACHE_BLOCK), (unsigned)(s.seqs * s.heads), 2);
+  const int wide = s.dim % 4 == 0 && (((uintptr_t)k | (uintptr_t)v) & 15) == 0;
+  hipLaunchKernelGGL(cache_read_kernel, grid, dim3(256), 0, st, s, CacheView(s, const_cast<void*>(cache)), tokens, wide, k, v);
 }
 
 // ---- the attention -------------------------------------------------------------------------------------------
@@ -153,15 +186,13 @@ __device__ __forceinline__ void cache_operand(uint32_t a, uint32_t b, Frag<bf16_
 }
 
 constexpr int ATTEND_WAVES = 8, ATTEND_CHUNK = 128, ATTEND_LD = ATTEND_CHUNK + 4;
-struct AttendPlan { int g_tiles, splits, per_split; };      // tiles of 16 queries; ranges of the tokens, of so many chunks of 128
+struct AttendPlan { int g_tiles, splits; };                 // tiles of 16 queries; ranges of the tokens
 static AttendPlan attend_plan(const CacheShape& s, int per, int q_heads, int tokens) {
   AttendPlan p;
   p.g_tiles = (per * (q_heads / s.heads) + 15) / 16;
   const long units = (long)s.seqs * s.heads * p.g_tiles;
   const int chunks = std::max(1, (tokens + ATTEND_CHUNK - 1) / ATTEND_CHUNK);
-  const int want = (int)std::min<long>(chunks, std::max<long>(1, 512 / units));
-  p.per_split = (chunks + want - 1) / want;
-  p.splits = (chunks + p.per_split - 1) / p.per_split;
+  p.splits = (int)std::min<long>(chunks, std::max<long>(1, 512 / units));
   return p;
 }
 size_t cache_attend_workspace(const CacheShape& s, int per, int q_heads, int tokens) {
@@ -172,7 +203,7 @@ size_t cache_attend_workspace(const CacheShape& s, int per, int q_heads, int tok
 
 struct AttendArgs {
   const void* q; size_t ldq; void* out; size_t ldo;
-  int per, share, splits, per_split, tokens, wide_q, wide_o;
+  int per, share, splits, tokens, wide_q;
   float scale;
   float* ml; float* part;                                    // of splits: (maximum, sum) [unit][split][16], products [unit][split][16][64 chunks]
 };
@@ -195,13 +226,31 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
   const int head = u % s.heads, b = u / s.heads;
   const int len = min(c.lengths[b], a.tokens);
   const int chunks = s.chunks(), E = chunks * 2;
-  const int first = split * a.per_split * ATTEND_CHUNK, last = min(len, first + a.per_split * ATTEND_CHUNK);
+  const int span = ((len + ATTEND_CHUNK - 1) / ATTEND_CHUNK + a.splits - 1) / a.splits * ATTEND_CHUNK;   // of this sequence: equal shares
+  const int first = split * span, last = min(len, first + span);
   const size_t at = ((size_t)b * s.heads + head) * s.blocks();
   const char* const kc = c.k + at * chunks * 2048;
   const char* const vc = c.v + at * chunks * 2048;
   const int q4 = lane >> 4, g = lane & 15;
   auto query = [&](int i) { return ((size_t)b * a.per + (g0 + i) / a.share); };   // row of query i of the tile
   auto column = [&](int i) { return (size_t)(head * a.share + (g0 + i) % a.share) * s.dim; };
+  const int ts = E >= 6 ? 1 : 8 / E, mine = E >= 6 ? w * EPW : w % E, my_ts = E >= 6 ? 0 : w / E;   // columns 32 mine.., tokens' share
+  v4f acc[EPW][2];
+#pragma unroll
+  for (int e = 0; e < EPW; ++e) acc[e][0] = acc[e][1] = v4f{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;                              // of query t / 32, in its 32 threads
+  // keys are asked for a chunk ahead, values before the chunk's scores are made: both are on their way in every phase
+  uint4 kr[4 * EPW], vr[4][EPW];
+  float ks = 0.f;
+  auto fetch_keys = [&](int t0) {
+    const int tile = t0 + 16 * w;
+    if (tile >= last) return;
+    const uint4* kp = reinterpret_cast<const uint4*>(kc + (size_t)(tile >> 4) * chunks * 1024) + lane;
+#pragma unroll
+    for (int ch = 0; ch < 4 * EPW; ++ch) if (ch < chunks) kr[ch] = kp[ch * 64];
+    ks = c.kscale[at + (tile >> 5)];
+  };
+  fetch_keys(first);
   if (first < last)
     for (int i = t; i < chunks * 128; i += 64 * ATTEND_WAVES) {   // the queries as operands: [chunk][half][part][lane]
       const int l = i & 63, ch = i >> 7, h = i >> 6 & 1, d = 64 * ch + 16 * (l >> 4) + 8 * h;
@@ -211,36 +260,40 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
 #pragma unroll
       for (int p = 0; p < QP; ++p) s_q[((ch * 2 + h) * QP + p) * 64 + l] = f[p].v;
     }
-  const int ts = E >= 6 ? 1 : 8 / E, mine = E >= 6 ? w * EPW : w % E, my_ts = E >= 6 ? 0 : w / E;   // columns 32 mine.., tokens' share
-  v4f acc[EPW][2];
-#pragma unroll
-  for (int e = 0; e < EPW; ++e) acc[e][0] = acc[e][1] = v4f{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;                              // of query t / 32, in its 32 threads
   __syncthreads();
   for (int t0 = first; t0 < last; t0 += ATTEND_CHUNK) {
-    const int tile = t0 + 16 * w;
-    if (tile < last) {
-      const uint4* kp = reinterpret_cast<const uint4*>(kc + (size_t)(tile >> 4) * chunks * 1024) + lane;
-      v4f z[2] = {v4f{0.f, 0.f, 0.f, 0.f}, v4f{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll 4
-      for (int ch = 0; ch < chunks; ++ch) {
-        const uint4 k = kp[ch * 64];
-        Frag<bf16_t> k0, k1, qf;
-        cache_operand(k.x, k.y, k0);
-        cache_operand(k.z, k.w, k1);
+    const int tok = t0 + 4 * (t & 31);
+    const float vs = tok < last ? c.vscale[at + (tok >> 5)] : 0.f;
 #pragma unroll
-        for (int p = QP - 1; p >= 0; --p) {
-          qf.v = s_q[(ch * 2 * QP + p) * 64 + lane]; mma16(z[0], k0, qf);
-          qf.v = s_q[((ch * 2 + 1) * QP + p) * 64 + lane]; mma16(z[1], k1, qf);
+    for (int i = 0; i < 4; ++i) {
+      const int blk = my_ts + i * ts;
+      if (blk >= ATTEND_CHUNK / CACHE_BLOCK || t0 + blk * CACHE_BLOCK >= last) break;
+      const uint4* vp = reinterpret_cast<const uint4*>(vc + (size_t)((t0 >> 5) + blk) * chunks * 2048) + lane;
+#pragma unroll
+      for (int e = 0; e < EPW; ++e) if (mine + e < E) vr[i][e] = vp[(mine + e) * 64];
+    }
+    if (t0 + 16 * w < last) {
+      v4f z[2] = {v4f{0.f, 0.f, 0.f, 0.f}, v4f{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int ch = 0; ch < 4 * EPW; ++ch)
+        if (ch < chunks) {
+          Frag<bf16_t> k0, k1, qf;
+          cache_operand(kr[ch].x, kr[ch].y, k0);
+          cache_operand(kr[ch].z, kr[ch].w, k1);
+#pragma unroll
+          for (int p = QP - 1; p >= 0; --p) {
+            qf.v = s_q[(ch * 2 * QP + p) * 64 + lane]; mma16(z[0], k0, qf);
+            qf.v = s_q[((ch * 2 + 1) * QP + p) * 64 + lane]; mma16(z[1], k1, qf);
+          }
         }
-      }
-      const float sc = c.kscale[at + (tile >> 5)] * a.scale;
+      const float sc = ks * a.scale;
       *reinterpret_cast<float4*>(s_s + g * ATTEND_LD + 16 * w + 4 * q4) =
           make_float4((z[0][0] + z[1][0]) * sc, (z[0][1] + z[1][1]) * sc, (z[0][2] + z[1][2]) * sc, (z[0][3] + z[1][3]) * sc);
     }
+    fetch_keys(t0 + ATTEND_CHUNK);
     __syncthreads();
     {
-      const int i = t >> 5, j = t & 31, tok = t0 + 4 * j;
+      const int i = t >> 5, j = t & 31;
       const float4 x4 = *reinterpret_cast<const float4*>(s_s + i * ATTEND_LD + 4 * j);
       float x[4] = {x4.x, x4.y, x4.z, x4.w}, mx = -INFINITY;
 #pragma unroll
@@ -249,7 +302,6 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
       for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
       const float mn = fmaxf(m, mx), ms = mn > -INFINITY ? mn : 0.f;
       const float f = m > -INFINITY ? (FAST ? __expf(m - ms) : expf(m - ms)) : 0.f;
-      const float vs = tok < last ? c.vscale[at + (tok >> 5)] : 0.f;
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -285,19 +337,19 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[e][h][i] *= f;
-    for (int blk = my_ts; blk < ATTEND_CHUNK / CACHE_BLOCK; blk += ts) {
-      if (t0 + blk * CACHE_BLOCK >= last) break;
-      const uint4* vp = reinterpret_cast<const uint4*>(vc + (size_t)((t0 >> 5) + blk) * chunks * 2048) + lane;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int blk = my_ts + i * ts;
+      if (blk >= ATTEND_CHUNK / CACHE_BLOCK || t0 + blk * CACHE_BLOCK >= last) break;
       Frag<bf16_t> pf[PP];
 #pragma unroll
       for (int p = 0; p < PP; ++p) pf[p].v = s_p[(blk * PP + p) * 64 + lane];
 #pragma unroll
       for (int e = 0; e < EPW; ++e)
         if (mine + e < E) {
-          const uint4 v = vp[(mine + e) * 64];
           Frag<bf16_t> v0, v1;
-          cache_operand(v.x, v.y, v0);
-          cache_operand(v.z, v.w, v1);
+          cache_operand(vr[i][e].x, vr[i][e].y, v0);
+          cache_operand(vr[i][e].z, vr[i][e].w, v1);
 #pragma unroll
           for (int p = PP - 1; p >= 0; --p) { mma16(acc[e][0], v0, pf[p]); mma16(acc[e][1], v1, pf[p]); }
         }
@@ -350,27 +402,53 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
           if (d + i < s.dim) out[d + i] = from_f<T>(acc[e][h][i] * inv);
       }
 }
-// joins the ranges of a query: one workgroup each
+// joins the ranges of a query: one workgroup each, its threads a column of four and a share of the ranges
+constexpr int ATTEND_SPLITS = 512;
 template <typename T>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a, CacheShape s) {
-  const int G = a.per * a.share, g_tiles = (G + 15) / 16;
+  __shared__ float s_w[ATTEND_SPLITS];
+  __shared__ float s_r[8];
+  __shared__ float4 s_o[256];
+  const int G = a.per * a.share, g_tiles = (G + 15) / 16, t = threadIdx.x, lane = t & 63, w = t >> 6;
   int u = blockIdx.x;
   const int g = u % G; u /= G;
   const int head = u % s.heads, b = u / s.heads;
   const size_t slot = ((size_t)(b * s.heads + head) * g_tiles + g / 16) * a.splits;
-  const float* ml = a.ml + (slot * 16 + g % 16) * 2;
-  float M = -INFINITY, L = 0.f;
-  for (int k = 0; k < a.splits; ++k) M = fmaxf(M, ml[k * 32]);
-  const float Ms = M > -INFINITY ? M : 0.f;
-  for (int k = 0; k < a.splits; ++k) if (ml[k * 32 + 1] != 0.f) L += ml[k * 32 + 1] * expf(ml[k * 32] - Ms);
-  const float inv = L == 0.f ? 0.f : 1.0f / L;
-  T* const out = (T*)a.out + ((size_t)b * a.per + g / a.share) * a.ldo + (size_t)(head * a.share + g % a.share) * s.dim;
-  const size_t ld = (size_t)s.chunks() * 64;
-  for (int d = threadIdx.x; d < s.dim; d += 256) {
-    float o = 0.f;
-    for (int k = 0; k < a.splits; ++k) if (ml[k * 32 + 1] != 0.f) o += a.part[((slot + k) * 16 + g % 16) * ld + d] * expf(ml[k * 32] - Ms);
-    out[d] = from_f<T>(o * inv);
+  const float2* ml = reinterpret_cast<const float2*>(a.ml) + slot * 16 + g % 16;
+  const float none = -INFINITY;
+  const float2 x0 = t < a.splits ? ml[t * 16] : make_float2(none, 0.f), x1 = t + 256 < a.splits ? ml[(t + 256) * 16] : make_float2(none, 0.f);
+  float most = wave_max(fmaxf(x0.x, x1.x));
+  if (lane == 0) s_r[w] = most;
+  __syncthreads();
+  most = fmaxf(fmaxf(s_r[0], s_r[1]), fmaxf(s_r[2], s_r[3]));
+  const float ms = most > none ? most : 0.f;
+  const float w0 = x0.y != 0.f ? expf(x0.x - ms) : 0.f, w1 = x1.y != 0.f ? expf(x1.x - ms) : 0.f;   // (a range without tokens: its products were not written)
+  if (t < a.splits) s_w[t] = w0;
+  if (t + 256 < a.splits) s_w[t + 256] = w1;
+  const float sum = wave_sum(x0.y * w0 + x1.y * w1);
+  if (lane == 0) s_r[4 + w] = sum;
+  __syncthreads();
+  const float all = s_r[4] + s_r[5] + s_r[6] + s_r[7], inv = all == 0.f ? 0.f : 1.0f / all;
+  const int cols = s.chunks() * 16, shares = 256 / cols, col = t % cols, share = t / cols;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (share < shares) {
+    const float4* p = reinterpret_cast<const float4*>(a.part) + (slot * 16 + g % 16) * cols + col;
+#pragma unroll 4
+    for (int k = share; k < a.splits; k += shares) {
+      const float f = s_w[k];
+      if (f == 0.f) continue;
+      const float4 x = p[(size_t)k * 16 * cols];
+      o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
+    }
   }
+  s_o[t] = o;
+  __syncthreads();
+  if (share) return;
+  for (int k = 1; k < shares; ++k) { const float4 x = s_o[k * cols + col]; o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w; }
+  T* const out = (T*)a.out + ((size_t)b * a.per + g / a.share) * a.ldo + (size_t)(head * a.share + g % a.share) * s.dim + 4 * col;
+  const float r[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) if (4 * col + e < s.dim) out[e] = from_f<T>(r[e]);
 }
 void launch_cache_attend(int prec, const CacheShape& s, const void* cache, const void* q, size_t ldq, int per, int q_heads, int tokens, float scale,
                          void* out, size_t ldo, void* workspace, hipStream_t st) {
@@ -378,7 +456,7 @@ void launch_cache_attend(int prec, const CacheShape& s, const void* cache, const
   const size_t es = prec ? 2 : 4;
   const long units = (long)s.seqs * s.heads * p.g_tiles;
   AttendArgs a{};
-  a.q = q; a.ldq = ldq; a.out = out; a.ldo = ldo; a.per = per; a.share = q_heads / s.heads; a.splits = p.splits; a.per_split = p.per_split;
+  a.q = q; a.ldq = ldq; a.out = out; a.ldo = ldo; a.per = per; a.share = q_heads / s.heads; a.splits = p.splits;
   a.tokens = tokens; a.scale = scale;
   a.wide_q = (((uintptr_t)q | ldq * es | s.dim * es) & 15) == 0;
   a.ml = (float*)workspace; a.part = a.ml + (size_t)units * p.splits * 32;

@@ -89,47 +89,56 @@ void launch_search_reorder(const ReorderJobs& jobs, int n, const int32_t* rows, 
 struct Parts3 { uint32_t h, m, l; };                       // bits as of an fp32, lower half 0
 __device__ __forceinline__ Parts3 parts3(float x) {
   const uint32_t u = __float_as_uint(x);
-  if ((u & 0x7f800000u) == 0x7f800000u) return {(u & 0x007fffffu) ? 0x7fc00000u : u, 0u, 0u};
+  const bool none = (u & 0x7f800000u) == 0x7f800000u;
   Parts3 p;
   p.h = u & 0xffff0000u;
   const float r = x - __uint_as_float(p.h);
   p.m = __float_as_uint(r) & 0xffff0000u;
-  p.l = __float_as_uint(r - __uint_as_float(p.m)) & 0xffff0000u;
+  p.l = none ? 0u : __float_as_uint(r - __uint_as_float(p.m)) & 0xffff0000u;
+  p.m = none ? 0u : p.m;
+  p.h = none && (u & 0x007fffffu) ? 0x7fc00000u : p.h;
   return p;
 }
 __device__ __forceinline__ uint32_t pack_hi(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }   // upper halves of both
 
-// 8 consecutive elements of x from k on (k < K: as many as there are, then 0) as operand parts: 1 of bf16, 3 of fp32.
+// Operand parts of 8 consecutive elements: 1 of bf16, 3 of fp32.
 template <typename T> constexpr int OPERAND_PARTS = sizeof(T) == 2 ? 1 : 3;
-__device__ __forceinline__ void load_operand(const bf16_t* p, int n, bool wide, Frag<bf16_t> (&f)[1]) {
-  if (n >= 8 && wide) { f[0].load(p); return; }
+// the first n (or all 8) elements at p, 0 behind them
+__device__ __forceinline__ void load_elements(const bf16_t* p, int n, Frag<bf16_t>& f) {
   uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (i < n) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
-  f[0].v = make_uint4(w[0], w[1], w[2], w[3]);
+  f.v = make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void split_operand(const float (&x)[8], Frag<bf16_t> (&f)[3]) {
+__device__ __forceinline__ void load_elements(const float* p, int n, Frag<float>& f) {
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : 0.f;
+  f.lo = make_float4(x[0], x[1], x[2], x[3]);
+  f.hi = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void operand_of(const Frag<bf16_t>& x, bool in, Frag<bf16_t> (&f)[1]) {   // in = false: zeros
+  f[0].v = make_uint4(in ? x.v.x : 0u, in ? x.v.y : 0u, in ? x.v.z : 0u, in ? x.v.w : 0u);
+}
+__device__ __forceinline__ void operand_of(const Frag<float>& x, bool in, Frag<bf16_t> (&f)[3]) {
   uint32_t h[4], m[4], l[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const Parts3 a = parts3(x[2 * i]), b = parts3(x[2 * i + 1]);
+    const Parts3 a = parts3(in ? x.get(2 * i) : 0.f), b = parts3(in ? x.get(2 * i + 1) : 0.f);
     h[i] = pack_hi(a.h, b.h); m[i] = pack_hi(a.m, b.m); l[i] = pack_hi(a.l, b.l);
   }
   f[0].v = make_uint4(h[0], h[1], h[2], h[3]);
   f[1].v = make_uint4(m[0], m[1], m[2], m[3]);
   f[2].v = make_uint4(l[0], l[1], l[2], l[3]);
 }
-__device__ __forceinline__ void load_operand(const float* p, int n, bool wide, Frag<bf16_t> (&f)[3]) {
-  float x[8];
-  if (n >= 8 && wide) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : 0.f;
-  }
-  split_operand(x, f);
+// the first n of 8 elements as operand parts; wide: p is a multiple of 16 bytes
+template <typename T>
+__device__ __forceinline__ void load_operand(const T* p, int n, bool wide, Frag<bf16_t> (&f)[OPERAND_PARTS<T>]) {
+  Frag<T> x;
+  if (n >= 8 && wide) x.load(p);
+  else load_elements(p, n, x);
+  operand_of(x, true, f);
 }
 
 }  // namespace cmt

@@ -105,11 +105,33 @@ void launch_quant_values(const void* packed, const QuantShape& q, float* out, hi
                      (const bf16_t*)((const char*)packed + q.code_bytes()), q, q.k_tiles(), out);
 }
 
+// four neighbouring outputs of row m; flags: 1 tanh, 2 y in bf16, 8 y takes them in one piece
+__device__ __forceinline__ void quant_store(float a, float b, float c, float d, int m, int n, int N, const float* __restrict__ bias, int flags,
+                                            void* __restrict__ y, size_t ldy) {
+  float r[4] = {a, b, c, d};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (bias && n + e < N) r[e] += bias[n + e];
+    if (flags & 1) r[e] = tanhf(r[e]);
+  }
+  if (flags & 2) {
+    bf16_t* o = (bf16_t*)y + (size_t)m * ldy + n;
+    if ((flags & 8) && n + 4 <= N) *reinterpret_cast<uint2*>(o) = make_uint2(f2bf(r[0]) | (uint32_t)f2bf(r[1]) << 16, f2bf(r[2]) | (uint32_t)f2bf(r[3]) << 16);
+    else
+      for (int e = 0; e < 4; ++e) if (n + e < N) o[e] = f2bf(r[e]);
+  } else {
+    float* o = (float*)y + (size_t)m * ldy + n;
+    if ((flags & 8) && n + 4 <= N) *reinterpret_cast<float4*>(o) = make_float4(r[0], r[1], r[2], r[3]);
+    else
+      for (int e = 0; e < 4; ++e) if (n + e < N) o[e] = r[e];
+  }
+}
+
 // ---- the product -------------------------------------------------------------------------------------------
 // A workgroup makes NT row blocks of the weight for CT tiles of 16 rows of x; its wavefronts split k, tile by tile, and add
 // up through LDS.  The weight is the instruction's first operand: a lane then holds 4 neighbouring outputs of one row of x.
 constexpr int QUANT_WAVES = 8;
-template <typename T, int GROUP, int NT, int CT>
+template <typename T, int GROUP, int NT, int CT, bool WHOLE>
 __global__ __launch_bounds__(64 * QUANT_WAVES) void quant_product_kernel(const T* __restrict__ x, size_t ldx, const uint4* __restrict__ codes,
                                                                          const bf16_t* __restrict__ scales, int M, int N, int K, int k_tiles,
                                                                          int row_blocks, int m_blocks, const float* __restrict__ bias, int flags,
@@ -121,7 +143,6 @@ __global__ __launch_bounds__(64 * QUANT_WAVES) void quant_product_kernel(const T
   const int id = blockIdx.x, seq = id >> 3, mb = seq % m_blocks, nb = ((seq / m_blocks) * 8 + (id & 7)) * NT;
   if (nb >= row_blocks) return;
   const int m0 = mb * 16 * CT, q = lane >> 4, c = lane & 15;
-  const bool wide = flags & 4;
   v4f acc[NT][CT];
 #pragma unroll
   for (int i = 0; i < NT; ++i)
@@ -144,7 +165,10 @@ __global__ __launch_bounds__(64 * QUANT_WAVES) void quant_product_kernel(const T
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const int k = kt * QUANT_TILE_K + 32 * s + 8 * q;
-        load_operand(x + (m < M ? (size_t)m * ldx + k : 0), m < M ? K - k : 0, wide, xf[j][s]);
+        Frag<T> f;
+        if constexpr (WHOLE) f.load(x + (size_t)min(m, M - 1) * ldx + (k < K ? k : 0));   // (rows beyond M: not stored)
+        else load_elements(x + (m < M ? (size_t)m * ldx + k : 0), m < M ? K - k : 0, f);
+        operand_of(f, !WHOLE || k < K, xf[j][s]);
       }
     }
 #pragma unroll
@@ -190,50 +214,209 @@ __global__ __launch_bounds__(64 * QUANT_WAVES) void quant_product_kernel(const T
     }
     const int m = m0 + 16 * (t % CT) + (l & 15), n = (nb + t / CT) * 16 + 4 * (l >> 4);
     if (m >= M || n >= N) continue;
-    float r[4] = {v.x, v.y, v.z, v.w};
+    quant_store(v.x, v.y, v.z, v.w, m, n, N, bias, flags, y, ldy);
+  }
+}
+
+// ---- many rows -----------------------------------------------------------------------------------------------
+// From some dozens of rows on the matrix instructions and the trips of x to the CUs bound the product, not the weights' read.  A workgroup
+// of 4 x 2 wavefronts makes 256 outputs for 32 MT rows: x comes through LDS, 128 k at a time and a tile ahead, in operand order; a
+// wavefront turns its 64 x 128 codes into operands once per tile (they stay in registers) and passes its MT tiles of rows by them.
+constexpr int QUANT_WIDE = 512;
+template <typename T, int GROUP, int MT, bool WHOLE>
+__global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T* __restrict__ x, size_t ldx, const uint4* __restrict__ codes,
+                                                                 const bf16_t* __restrict__ scales, int M, int N, int K, int k_tiles, int row_blocks,
+                                                                 int m_blocks, const float* __restrict__ bias, int flags, void* __restrict__ y,
+                                                                 size_t ldy) {
+  constexpr int PARTS = OPERAND_PARTS<T>, PER = QUANT_TILE_K / GROUP, STEPS = GROUP / 32, WN = 4, NT = 4;
+  constexpr bool DIRECT = WHOLE && sizeof(T) == 2;
+  constexpr int THREADS = QUANT_WIDE, SLOTS = 2 * MT * 4 * 64, MINE = SLOTS / THREADS;   // 16 bytes (a part) of x each: [tile of rows][step][lane]
+  __shared__ uint4 xs[2][PARTS][SLOTS];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wn = w >> 1, wm = w & 1;
+  const int id = blockIdx.x, seq = id >> 3, mb = seq % m_blocks, nb = ((seq / m_blocks) * 8 + (id & 7)) * NT * WN + wn * NT;
+  if (nb - wn * NT >= row_blocks) return;
+  const int m0 = mb * 32 * MT, q = lane >> 4, c = lane & 15;
+  v4f acc[NT][MT];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (bias && n + e < N) r[e] += bias[n + e];
-      if (flags & 1) r[e] = tanhf(r[e]);
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+  const uint4* cp[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) cp[i] = codes + (size_t)min(nb + i, row_blocks - 1) * k_tiles * 64 + lane;
+  Frag<T> xn[MINE];                                          // as they come: nothing waits for them before they go to LDS
+  uint4 code[NT];
+  uint2 sn[NT][PER];
+  const bf16_t* const sp = scales + 4 * q;
+  // 16-bit rows of whole pieces go from memory to LDS without passing registers (the instruction is written out because the compiler would
+  // wait for it before the next read of LDS); the last tile's pieces behind K are zeros.
+  unsigned off[MINE];
+  const char* const xb = (const char*)(x + (size_t)m0 * ldx);
+  if constexpr (DIRECT) {
+#pragma unroll
+    for (int u = 0; u < MINE; ++u) {
+      const int slot = u * THREADS + threadIdx.x, l = slot & 63, m = min(m0 + 16 * (slot >> 8) + (l & 15), M - 1) - m0;
+      off[u] = ((unsigned)m * (unsigned)ldx + 32 * (slot >> 6 & 3) + 8 * (l >> 4)) * 2;
     }
-    if (flags & 2) {
-      bf16_t* d = (bf16_t*)y + (size_t)m * ldy + n;
-      if ((flags & 8) && n + 4 <= N) *reinterpret_cast<uint2*>(d) = make_uint2(f2bf(r[0]) | (uint32_t)f2bf(r[1]) << 16, f2bf(r[2]) | (uint32_t)f2bf(r[3]) << 16);
-      else
-        for (int e = 0; e < 4; ++e) if (n + e < N) d[e] = f2bf(r[e]);
+  }
+  auto request = [&](int kt, uint4* to) {
+    const char* const src = xb + (size_t)kt * QUANT_TILE_K * 2;
+    if ((kt + 1) * QUANT_TILE_K <= K) {
+#pragma unroll
+      for (int u = 0; u < MINE; ++u) {
+        const unsigned dst = (unsigned)(size_t)(__attribute__((address_space(3))) const char*)(to + u * THREADS + w * 64);
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off[u]), "s"(src) : "memory");
+      }
     } else {
-      float* d = (float*)y + (size_t)m * ldy + n;
-      if ((flags & 8) && n + 4 <= N) *reinterpret_cast<float4*>(d) = make_float4(r[0], r[1], r[2], r[3]);
-      else
-        for (int e = 0; e < 4; ++e) if (n + e < N) d[e] = r[e];
+#pragma unroll
+      for (int u = 0; u < MINE; ++u) {
+        const int slot = u * THREADS + threadIdx.x;
+        const bool in = kt * QUANT_TILE_K + 32 * (slot >> 6 & 3) + 8 * (slot >> 4 & 3) < K;
+        to[slot] = in ? *reinterpret_cast<const uint4*>(src + off[u]) : make_uint4(0, 0, 0, 0);
+      }
+    }
+  };
+  auto fetch = [&](int kt) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      code[i] = cp[i][(size_t)kt * 64];
+#pragma unroll
+      for (int g = 0; g < PER; ++g)
+        sn[i][g] = *reinterpret_cast<const uint2*>(sp + (((size_t)min(nb + i, row_blocks - 1) * k_tiles + kt) * PER + g) * 16);
+    }
+    if constexpr (DIRECT) return;
+#pragma unroll
+    for (int u = 0; u < MINE; ++u) {
+      const int slot = u * THREADS + threadIdx.x, l = slot & 63, s = slot >> 6 & 3, m = m0 + 16 * (slot >> 8) + (l & 15);
+      const int k = kt * QUANT_TILE_K + 32 * s + 8 * (l >> 4);
+      if constexpr (WHOLE) xn[u].load(x + (size_t)min(m, M - 1) * ldx + (k < K ? k : 0));   // (rows beyond M: not stored)
+      else load_elements(x + (m < M ? (size_t)m * ldx + k : 0), m < M ? K - k : 0, xn[u]);
+    }
+  };
+  if constexpr (DIRECT) request(0, xs[0][0]);
+  fetch(0);
+  for (int kt = 0; kt < k_tiles; ++kt) {
+    uint4 (&buf)[PARTS][SLOTS] = xs[kt & 1];
+    if constexpr (!DIRECT)
+#pragma unroll
+    for (int u = 0; u < MINE; ++u) {
+      const int slot = u * THREADS + threadIdx.x;
+      Frag<bf16_t> f[PARTS];
+      operand_of(xn[u], !WHOLE || kt * QUANT_TILE_K + 32 * (slot >> 6 & 3) + 8 * (slot >> 4 & 3) < K, f);
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) buf[p][slot] = f[p].v;
+    }
+    Frag<bf16_t> wf[NT][4];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) quant_operand((&code[i].x)[s], wf[i][s]);
+    uint2 sc[NT][PER];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int g = 0; g < PER; ++g)
+        sc[i][g] = sn[i][g];
+    if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (kt + 1 < k_tiles) {
+      if constexpr (DIRECT) request(kt + 1, xs[(kt + 1) & 1][0]);
+      fetch(kt + 1);
+    }
+    // the next step's x is asked of LDS before a step's products begin
+    constexpr int SEQ = MT * 4;
+    Frag<bf16_t> xf[2][PARTS];
+    auto read = [&](int i, Frag<bf16_t> (&f)[PARTS]) {
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) f[p].v = buf[p][(wm * SEQ + i) * 64 + lane];
+    };
+    read(0, xf[0]);
+    v4f part[NT];
+#pragma unroll
+    for (int i = 0; i < SEQ; ++i) {
+      const int j = i >> 2, s = i & 3, g = s / STEPS;
+      if (i + 1 < SEQ) read(i + 1, xf[(i + 1) & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (s % STEPS == 0)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) part[n] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma16(part[n], wf[n][s], xf[i & 1][p]);
+      if (s % STEPS == STEPS - 1)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          acc[n][j][0] = fmaf(part[n][0], __uint_as_float(sc[n][g].x << 16), acc[n][j][0]);
+          acc[n][j][1] = fmaf(part[n][1], __uint_as_float(sc[n][g].x & 0xffff0000u), acc[n][j][1]);
+          acc[n][j][2] = fmaf(part[n][2], __uint_as_float(sc[n][g].y << 16), acc[n][j][2]);
+          acc[n][j][3] = fmaf(part[n][3], __uint_as_float(sc[n][g].y & 0xffff0000u), acc[n][j][3]);
+        }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int n = (nb + i) * 16 + 4 * q;
+    if (n >= N) continue;
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+      const int m = m0 + 16 * (wm * MT + j) + c;
+      if (m < M) quant_store(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], m, n, N, bias, flags, y, ldy);
     }
   }
 }
+
 template <typename T, int GROUP, int NT, int CT>
 static void quant_product_go(const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, int flags, void* y, size_t ldy, hipStream_t st) {
   const QuantShape& q = w.shape;
   const int m_blocks = (M + 16 * CT - 1) / (16 * CT);
   const int n_blocks = ((q.row_blocks() + NT - 1) / NT + 7) / 8 * 8;
-  hipLaunchKernelGGL((quant_product_kernel<T, GROUP, NT, CT>), dim3((unsigned)n_blocks * m_blocks), dim3(64 * QUANT_WAVES), 0, st, (const T*)x, ldx,
-                     (const uint4*)w.packed, (const bf16_t*)(w.packed + q.code_bytes()), M, q.N, q.K, q.k_tiles(), q.row_blocks(), m_blocks, bias, flags,
-                     y, ldy);
+  auto* kernel = flags & 4 ? quant_product_kernel<T, GROUP, NT, CT, true> : quant_product_kernel<T, GROUP, NT, CT, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)n_blocks * m_blocks), dim3(64 * QUANT_WAVES), 0, st, (const T*)x, ldx, (const uint4*)w.packed,
+                     (const bf16_t*)(w.packed + q.code_bytes()), M, q.N, q.K, q.k_tiles(), q.row_blocks(), m_blocks, bias, flags, y, ldy);
 }
+template <typename T, int GROUP, int MT>
+static void quant_product_wide_go(const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, int flags, void* y, size_t ldy,
+                                  hipStream_t st) {
+  const QuantShape& q = w.shape;
+  const int m_blocks = (M + 32 * MT - 1) / (32 * MT), n_blocks = ((q.row_blocks() + 15) / 16 + 7) / 8 * 8;
+  auto* kernel = flags & 4 ? quant_product_wide_kernel<T, GROUP, MT, true> : quant_product_wide_kernel<T, GROUP, MT, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)n_blocks * m_blocks), dim3(QUANT_WIDE), 0, st, (const T*)x, ldx, (const uint4*)w.packed,
+                     (const bf16_t*)(w.packed + q.code_bytes()), M, q.N, q.K, q.k_tiles(), q.row_blocks(), m_blocks, bias, flags, y, ldy);
+}
+// Which kernel and tile, by sizes alone; times are of whole calls, us, 11 of them the host's (bf16 unless said).
+//   Many rows: k is not split there, so it takes workgroups of 64 rows for most of the chip.  32000 x 1024, groups of 128 | 32: 64 rows
+//   15 | 23 with k split against 17 | 26, 96 rows 21 | 32 against 19 | 27, 640 rows 108 | 187 against 78 | 116; 4096 x 2048, 640 rows (160
+//   workgroups) 27 | 42 against 30 | 44.  More rows to a workgroup (as many as a wavefront's registers hold the sums of beside the
+//   scales of its groups: 160 rows with groups of 128, 128 of 64) where rounds of workgroups times their rows are fewer: 640 rows 62 against 78, 128 rows 28 against 18.
+//   Else two tiles of rows to a workgroup where there are two (640 rows 108 against 129; fp32, whose parts are three times the registers, 285
+//   against 226: one), and four row blocks of the weight, which share x, where one each would be 512 workgroups or more (4096 x 2048, 128 rows
+//   11 against 18; 512 x 4096 in fp32, 128 rows 17 against 12).
 template <typename T, int GROUP>
 static void quant_product_tiles(const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, int flags, void* y, size_t ldy,
                                 hipStream_t st) {
-  const int rb = w.shape.row_blocks();
-  if (M <= 16) {
-    if (rb <= 512) quant_product_go<T, GROUP, 1, 1>(x, ldx, w, M, bias, flags, y, ldy, st);
-    else quant_product_go<T, GROUP, 4, 1>(x, ldx, w, M, bias, flags, y, ldy, st);
-  } else {
-    if (rb <= 512) quant_product_go<T, GROUP, 1, 2>(x, ldx, w, M, bias, flags, y, ldy, st);
-    else quant_product_go<T, GROUP, 4, 2>(x, ldx, w, M, bias, flags, y, ldy, st);
+  constexpr int MOST = sizeof(T) == 4 || GROUP == 32 ? 2 : GROUP == 64 ? 4 : 5, CT = sizeof(T) == 4 ? 1 : 2;
+  const long rb = w.shape.row_blocks();
+  auto wgs = [&](int mt) { return (rb + 15) / 16 * ((M + 32 * mt - 1) / (32 * mt)); };
+  if (M > 64 && wgs(2) >= 200) {
+    if constexpr (MOST > 2)
+      if ((wgs(MOST) + 255) / 256 * (MOST + 1) <= (wgs(2) + 255) / 256 * 3) { quant_product_wide_go<T, GROUP, MOST>(x, ldx, w, M, bias, flags, y, ldy, st); return; }
+    quant_product_wide_go<T, GROUP, 2>(x, ldx, w, M, bias, flags, y, ldy, st);
+    return;
   }
+  if constexpr (CT > 1)
+    if (M > 16) {
+      if (rb * ((M + 31) / 32) < 512) quant_product_go<T, GROUP, 1, CT>(x, ldx, w, M, bias, flags, y, ldy, st);
+      else quant_product_go<T, GROUP, 4, CT>(x, ldx, w, M, bias, flags, y, ldy, st);
+      return;
+    }
+  if (rb * ((M + 15) / 16) < 512) quant_product_go<T, GROUP, 1, 1>(x, ldx, w, M, bias, flags, y, ldy, st);
+  else quant_product_go<T, GROUP, 4, 1>(x, ldx, w, M, bias, flags, y, ldy, st);
 }
 void launch_quant_product(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, bool tanh, int y_prec, void* y,
                           size_t ldy, hipStream_t st) {
   const size_t xs = prec ? 2 : 4, ys = y_prec ? 2 : 4;
-  const int flags = (tanh ? 1 : 0) | (y_prec ? 2 : 0) | (((uintptr_t)x | ldx * xs) % 16 == 0 ? 4 : 0) | (((uintptr_t)y | ldy * ys) % (4 * ys) == 0 ? 8 : 0);
+  const int flags = (tanh ? 1 : 0) | (y_prec ? 2 : 0) | (((uintptr_t)x | ldx * xs) % 16 == 0 && w.shape.K % 8 == 0 && ldx <= 1 << 20 ? 4 : 0) | (((uintptr_t)y | ldy * ys) % (4 * ys) == 0 ? 8 : 0);
   auto go = [&](auto type) {
     using T = decltype(type);
     if (w.shape.group == 32) quant_product_tiles<T, 32>(x, ldx, w, M, bias, flags, y, ldy, st);

@@ -7,11 +7,12 @@ a tensor that wants a gradient is refused.  There is no CPU fallback."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 
 import torch
 
 from . import binding
-from .binding import CMT_OK, CmtCacheConfig, CmtCacheRows, CmtError, CmtReorderTensor
+from .binding import CMT_OK, CmtCacheConfig, CmtCacheRows, CmtError
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
@@ -42,21 +43,16 @@ def _pitch(t):
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-class _On:
-    """The device of the tensors as the current one, and its current stream."""
-
-    def __init__(self, device):
-        self.device, self.other = device, None
-
-    def __enter__(self):
-        if self.device.index != torch.cuda.current_device():
-            self.other = torch.cuda.device(self.device)
-            self.other.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream
-
-    def __exit__(self, *error):
-        if self.other is not None:
-            self.other.__exit__(*error)
+def _call(f, device, *args):
+    """f(*args, stream) with the tensors' device as the current one and its current stream.  (torch's own way to the
+    stream's handle builds a Stream object for it: 1.9 us of the 4 that a launch takes.)"""
+    if device.index == torch.cuda.current_device():
+        rc = f(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    else:
+        with torch.cuda.device(device):
+            rc = f(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if rc != CMT_OK:
+        _check(rc)
 
 
 class QuantWeight:
@@ -77,9 +73,8 @@ class QuantWeight:
         """From a weight [outputs, inputs] in fp32 or bf16: scale = bf16(max|w| / 6) and the nearest codes."""
         _tensor(weight, "weight", (2,), _TYPES)
         w = cls(*weight.shape, group, weight.device)
-        with _On(w.device) as stream:
-            _check(binding.load_library().cmt_quant_weight_pack(weight.data_ptr(), _TYPES[weight.dtype], _pitch(weight), w.outputs, w.inputs, group,
-                                                                w.packed.data_ptr(), stream))
+        _call(binding.load_library().cmt_quant_weight_pack, w.device, weight.data_ptr(), _TYPES[weight.dtype], _pitch(weight), w.outputs, w.inputs,
+              group, w.packed.data_ptr())
         return w
 
     @classmethod
@@ -92,16 +87,14 @@ class QuantWeight:
             raise ValueError(f"scales must be {(w.outputs, -(-w.inputs // group))}, not {tuple(scales.shape)}")
         if not codes.is_contiguous() or not scales.is_contiguous():
             raise ValueError("codes and scales must be contiguous")
-        with _On(w.device) as stream:
-            _check(binding.load_library().cmt_quant_weight_encode(codes.data_ptr(), scales.data_ptr(), w.outputs, w.inputs, group, w.packed.data_ptr(),
-                                                                  stream))
+        _call(binding.load_library().cmt_quant_weight_encode, w.device, codes.data_ptr(), scales.data_ptr(), w.outputs, w.inputs, group,
+              w.packed.data_ptr())
         return w
 
     def values(self):
         """The weight that the codes stand for, fp32 [outputs, inputs]."""
         out = torch.empty(self.outputs, self.inputs, dtype=torch.float32, device=self.device)
-        with _On(self.device) as stream:
-            _check(binding.load_library().cmt_quant_weight_values(self.packed.data_ptr(), self.outputs, self.inputs, self.group, out.data_ptr(), stream))
+        _call(binding.load_library().cmt_quant_weight_values, self.device, self.packed.data_ptr(), self.outputs, self.inputs, self.group, out.data_ptr())
         return out
 
 
@@ -126,10 +119,8 @@ def quant_product(x, weight, bias=None, tanh=False, out_dtype=None, out=None):
         if tuple(out.shape) != (rows, weight.outputs):
             raise ValueError(f"out must be {(rows, weight.outputs)}, not {tuple(out.shape)}")
         _apart(out, "out", x, "x")
-    with _On(x.device) as stream:
-        _check(binding.load_library().cmt_quant_product(
-            x.data_ptr(), _TYPES[x.dtype], _pitch(x), rows, weight.packed.data_ptr(), weight.outputs, weight.inputs, weight.group,
-            None if bias is None else bias.data_ptr(), bool(tanh), out.data_ptr(), _TYPES[out.dtype], _pitch(out), stream))
+    _call(binding.load_library().cmt_quant_product, x.device, x.data_ptr(), _TYPES[x.dtype], _pitch(x), rows, weight.packed.data_ptr(), weight.outputs,
+          weight.inputs, weight.group, None if bias is None else bias.data_ptr(), bool(tanh), out.data_ptr(), _TYPES[out.dtype], _pitch(out))
     return out
 
 
@@ -173,9 +164,7 @@ class SourceCache:
         if lengths.shape[0] != self.sequences:
             raise ValueError(f"lengths must have {self.sequences} elements, not {lengths.shape[0]}")
         rows = [CmtCacheRows(t.data_ptr(), *t.stride()[:3]) for t in (keys, values)]
-        with _On(self.device) as stream:
-            _check(binding.load_library().cmt_cache_fill(C.byref(self.config), self.data.data_ptr(), C.byref(rows[0]), C.byref(rows[1]),
-                                                         _TYPES[keys.dtype], lengths.data_ptr(), want[1], stream))
+        _call(binding.load_library().cmt_cache_fill, self.device, self.config, self.data.data_ptr(), *rows, _TYPES[keys.dtype], lengths.data_ptr(), want[1])
         self.tokens = want[1]
         return self
 
@@ -184,9 +173,7 @@ class SourceCache:
         self._filled()
         keys = torch.empty(self.sequences, self.tokens, self.heads, self.head_dim, dtype=torch.float32, device=self.device)
         values = torch.empty_like(keys)
-        with _On(self.device) as stream:
-            _check(binding.load_library().cmt_cache_read(C.byref(self.config), self.data.data_ptr(), self.tokens, keys.data_ptr(), values.data_ptr(),
-                                                         stream))
+        _call(binding.load_library().cmt_cache_read, self.device, self.config, self.data.data_ptr(), self.tokens, keys.data_ptr(), values.data_ptr())
         return keys, values
 
     def attend(self, query, scale=1.0, out=None):
@@ -215,17 +202,22 @@ class SourceCache:
             size = C.c_size_t()
             _check(lib.cmt_cache_attend_workspace(C.byref(self.config), per, heads, self.tokens, C.byref(size)))
             need = self._needs[key] = size.value
-        with _On(self.device) as stream:
-            work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-            _check(lib.cmt_cache_attend(
-                C.byref(self.config), self.data.data_ptr(), query.data_ptr(), _TYPES[query.dtype], query.stride(0) if rows > 1 else heads * dim, per,
-                heads, self.tokens, scale, out.data_ptr(), out.stride(0) if rows > 1 else heads * dim, None if work is None else work.data_ptr(), need,
-                stream))
+        work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        _call(lib.cmt_cache_attend, self.device, self.config, self.data.data_ptr(), query.data_ptr(), _TYPES[query.dtype],
+              query.stride(0) if rows > 1 else heads * dim, per, heads, self.tokens, scale, out.data_ptr(), out.stride(0) if rows > 1 else heads * dim,
+              None if work is None else work.data_ptr(), need)
         return out
 
     def _filled(self):
         if not self.tokens:
             raise ValueError("the cache has not been filled")
+
+
+@functools.lru_cache(maxsize=256)
+def _select_workspace(sentences, beam, vocab):
+    size = C.c_size_t()
+    _check(binding.load_library().cmt_beam_select_workspace(sentences, beam, vocab, C.byref(size)))
+    return size.value
 
 
 def beam_select(logits, scores, n=None):
@@ -240,15 +232,15 @@ def beam_select(logits, scores, n=None):
         raise ValueError(f"logits have {logits.shape[0]} rows, scores {sentences} x {beam} places")
     if not scores.is_contiguous():
         raise ValueError("scores must be contiguous")
-    n, lib, vocab = beam if n is None else n, binding.load_library(), logits.shape[1]
-    size = C.c_size_t()
-    _check(lib.cmt_beam_select_workspace(sentences, beam, vocab, C.byref(size)))
-    with _On(logits.device) as stream:
-        new = torch.empty((sentences, n), dtype=torch.float32, device=logits.device)
-        rows, tokens = torch.empty((2, sentences, n), dtype=torch.int32, device=logits.device).unbind(0)
-        work = torch.empty(size.value, dtype=torch.uint8, device=logits.device)
-        _check(lib.cmt_beam_select(logits.data_ptr(), _TYPES[logits.dtype], _pitch(logits), scores.data_ptr(), sentences, beam, vocab, n,
-                                   new.data_ptr(), rows.data_ptr(), tokens.data_ptr(), work.data_ptr(), size.value, stream))
+    n, vocab, device = beam if n is None else n, logits.shape[1], logits.device
+    need = _select_workspace(sentences, beam, vocab)
+    if not isinstance(n, int) or n < 1:
+        raise ValueError(f"n must be a positive number, not {n!r}")
+    new = torch.empty((sentences, n), dtype=torch.float32, device=device)
+    rows, tokens = torch.empty((2, sentences, n), dtype=torch.int32, device=device).unbind(0)
+    work = torch.empty(need, dtype=torch.uint8, device=device)
+    _call(binding.load_library().cmt_beam_select, device, logits.data_ptr(), _TYPES[logits.dtype], _pitch(logits), scores.data_ptr(), sentences, beam,
+          vocab, n, new.data_ptr(), rows.data_ptr(), tokens.data_ptr(), work.data_ptr(), need)
     return new, rows, tokens
 
 
@@ -257,29 +249,35 @@ def beam_reorder(rows, sources, targets):
     tensors' first dimension counting rows, the others contiguous.  Target rows whose number is outside the source stay as they were."""
     if not isinstance(rows, torch.Tensor) or rows.dtype != torch.int32 or not rows.is_contiguous() or not rows.is_cuda:
         raise ValueError("rows must be a contiguous int32 tensor on a GPU")
-    if len(sources) != len(targets):
-        raise ValueError(f"{len(sources)} sources and {len(targets)} targets")
-    count, source_rows = rows.numel(), sources[0].shape[0] if sources else 0
-    jobs = (CmtReorderTensor * len(sources))()
-    for i, (a, b) in enumerate(zip(sources, targets)):
-        if a.dtype != b.dtype or a.device != rows.device or b.device != rows.device:
-            raise ValueError(f"tensors {i} must be of one type and on the device of rows")
-        if a.dim() == 0 or a.shape[1:] != b.shape[1:] or a.shape[0] != source_rows or b.shape[0] != count:
-            raise ValueError(f"tensors {i} must have {source_rows} and {count} rows alike, not {tuple(a.shape)} and {tuple(b.shape)}")
-        if (a.requires_grad or b.requires_grad) and torch.is_grad_enabled():
-            raise ValueError(f"tensors {i} want a gradient: these operators have none (use torch.no_grad())")
-        size, width = a.element_size(), 1
-        for t in (a, b):
-            width = 1
-            for d in range(t.dim() - 1, 0, -1):
-                if t.shape[d] > 1 and t.stride(d) != width:
-                    raise ValueError(f"tensors {i}: the elements of a row must lie side by side")
-                width *= t.shape[d]
-        job = jobs[i]
-        job.source, job.target, job.row_bytes = a.data_ptr(), b.data_ptr(), width * size
-        job.source_pitch = (a.stride(0) if a.shape[0] > 1 else width) * size
-        job.target_pitch = (b.stride(0) if b.shape[0] > 1 else width) * size
-    if not sources or not count or not source_rows:
+    if len(sources) != len(targets) or not all(isinstance(t, torch.Tensor) and t.dim() for t in (*sources, *targets)):
+        raise ValueError("sources and targets must be as many tensors, of one dimension at least")
+    if not sources:
         return
-    with _On(rows.device) as stream:
-        _check(binding.load_library().cmt_beam_reorder(rows.data_ptr(), count, source_rows, jobs, len(sources), stream))
+    count, source_rows, device, grad = rows.numel(), len(sources[0]), rows.device, torch.is_grad_enabled()
+    fields = []                                            # of a CmtReorderTensor each: five numbers of 64 bits
+    for i, (a, b) in enumerate(zip(sources, targets)):
+        sa, sb = a.shape, b.shape
+        if sa[0] != source_rows or sb[0] != count or (sa != sb if count == source_rows else sa[1:] != sb[1:]):
+            raise ValueError(f"tensors {i} must have {source_rows} and {count} rows alike, not {tuple(sa)} and {tuple(sb)}")
+        if a.dtype != b.dtype or a.device != device or b.device != device:
+            raise ValueError(f"tensors {i} must be of one type and on the device of rows")
+        if grad and (a.requires_grad or b.requires_grad):
+            raise ValueError(f"tensors {i} want a gradient: these operators have none (use torch.no_grad())")
+        size = a.element_size()
+        width = a.numel() // source_rows * size if source_rows else 0
+        if width:
+            fields += (a.data_ptr(), b.data_ptr(), width if a.is_contiguous() else _row_pitch(a, i) * size,
+                       width if b.is_contiguous() else _row_pitch(b, i) * size, width)
+    if not fields or not count:
+        return
+    _call(binding.load_library().cmt_beam_reorder, device, rows.data_ptr(), count, source_rows, (C.c_int64 * len(fields))(*fields), len(fields) // 5)
+
+
+def _row_pitch(t, i):
+    """Elements from one row (first dimension) to the next, whose own elements lie side by side."""
+    side = 1
+    for d in range(t.dim() - 1, 0, -1):
+        if t.shape[d] > 1 and t.stride(d) != side:
+            raise ValueError(f"tensors {i}: the elements of a row must lie side by side")
+        side *= t.shape[d]
+    return t.stride(0) if t.shape[0] > 1 else side
