@@ -21,27 +21,16 @@ __device__ __forceinline__ float cache_code(float x, float s, float inv) {
 }
 
 // ---- writing ---------------------------------------------------------------------------------------------
-constexpr int FILL_PAD = 16;
 template <typename T>
-__device__ __forceinline__ void fill_load(const T* p, int n, bool wide, float (&x)[16]) {
-  if (n >= 16 && wide) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      Frag<T> f;
-      f.load(p + 8 * h);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[8 * h + i] = f.get(i);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = i < n ? to_f(p[i]) : 0.f;
-  }
+__device__ __forceinline__ void fill_load(const T* p, int n, bool wide, Frag<T> (&x)[2]) {   // the first n of 16 elements, then 0
+  if (n >= 16 && wide) { x[0].load(p); x[1].load(p + 8); }
+  else { load_elements(p, n, x[0]); load_elements(p + 8, n - 8, x[1]); }
 }
 // One workgroup per block of 32 tokens, sequence and head; blockIdx.z: keys, values.  The block is read once: a thread keeps its NS
 // slots of 16 d of a token until the scale is known.
 template <typename T, int NS>
 __global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const int32_t* __restrict__ lengths, int tokens, CacheShape s, CacheView c, int wide) {
-  __shared__ __align__(16) int8_t code[CACHE_BLOCK * (256 * NS + FILL_PAD)];
+  __shared__ uint4 code[512 * NS];                           // values: in the cache's order
   __shared__ float s_most[8];
   __shared__ int s_bad[8];
   const int b = blockIdx.y / s.heads, head = blockIdx.y % s.heads, blk = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
@@ -53,9 +42,10 @@ __global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const 
   const size_t tok = is_v ? src.v_tok : src.k_tok;
   const T* p = (const T*)(is_v ? src.v : src.k) + (size_t)b * (is_v ? src.v_seq : src.k_seq) + (size_t)head * (is_v ? src.v_head : src.k_head) +
                (size_t)blk * CACHE_BLOCK * tok;
-  const int chunks = s.chunks(), ld = chunks * 64 + FILL_PAD, slots = chunks * 128;   // at most 512 NS
+  const int chunks = s.chunks(), slots = chunks * 128;       // at most 512 NS
   const bool wd = wide >> is_v & 1;
-  float x[NS][16], most = 0.f;
+  Frag<T> x[NS][2];                                          // as they come: 16-bit ones take half the registers
+  float most = 0.f;
   bool bad = false;
 #pragma unroll
   for (int k = 0; k < NS; ++k) {
@@ -65,8 +55,12 @@ __global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const 
 #pragma unroll
   for (int k = 0; k < NS; ++k)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) { most = fmaxf(most, fabsf(x[k][e])); bad |= !(fabsf(x[k][e]) <= 3.4028235e38f); }
-  most = wave_max(most);
+    for (int e = 0; e < 16; ++e) {
+      const float a = fabsf(x[k][e >> 3].get(e & 7));
+      most = fmaxf(most, a);
+      bad |= !(a <= 3.4028235e38f);
+    }
+  most = lanes_max(most);
   const bool any = __ballot(bad) != 0;
   if (lane == 0) { s_most[w] = most; s_bad[w] = any; }
   __syncthreads();
@@ -78,45 +72,58 @@ __global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const 
   if (t == 0) (is_v ? c.vscale : c.kscale)[at] = scale;
   const bool some = scale > 0.f, tiny = scale < 1e-36f;
   const float inv = 1.0f / scale;
+  char* const out = (is_v ? c.v : c.k) + at * chunks * 2048;
 #pragma unroll
   for (int k = 0; k < NS; ++k) {
-    const int i = k * 512 + t, r = (i & 15) + 16 * (i >> 6 & 1), d = 64 * (i >> 7) + 16 * (i >> 4 & 3);
+    const int i = k * 512 + t;
     uint32_t o[4] = {0, 0, 0, 0};
     if (tiny && some) {                                      // (uniform; 1 / scale may be infinite)
 #pragma unroll 1
       for (int e = 0; e < 16; ++e) {
         float y = 0.f;
 #pragma unroll
-        for (int f = 0; f < 16; ++f) y = f == e ? x[k][f] : y;
+        for (int f = 0; f < 16; ++f) y = f == e ? x[k][f >> 3].get(f & 7) : y;
         const uint32_t q = (uint32_t)((int)fmin(fmax(rint((double)y / (double)scale), -127.0), 127.0) & 255) << (8 * (e & 3));
 #pragma unroll
         for (int f = 0; f < 4; ++f) o[f] |= f == e >> 2 ? q : 0u;
       }
     } else if (some) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[e >> 2] |= (uint32_t)((int)cache_code(x[k][e], scale, inv) & 255) << (8 * (e & 3));
+      for (int e = 0; e < 16; ++e) o[e >> 2] |= (uint32_t)((int)cache_code(x[k][e >> 3].get(e & 7), scale, inv) & 255) << (8 * (e & 3));
     }
-    if (i < slots) *reinterpret_cast<uint4*>(code + r * ld + d) = make_uint4(o[0], o[1], o[2], o[3]);
-  }
-  __syncthreads();
-  char* out = (is_v ? c.v : c.k) + at * chunks * 2048;
-  if (!is_v) {
-    for (int i = t; i < slots; i += 512) {                   // [16-token tile][chunk][lane]
-      const int tile = i / (chunks * 64), rest = i - tile * chunks * 64, ch = rest >> 6, l = rest & 63;
-      *reinterpret_cast<uint4*>(out + (size_t)i * 16) = *reinterpret_cast<const uint4*>(code + (16 * tile + (l & 15)) * ld + 64 * ch + 16 * (l >> 4));
+    if (!is_v) {                                             // a slot is a lane's 16 bytes: [16-token tile][chunk][lane]
+      if (i < slots) *reinterpret_cast<uint4*>(out + ((size_t)((i >> 6 & 1) * chunks + (i >> 7)) * 64 + (i & 63)) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+      continue;
     }
-  } else {
-    for (int i = t; i < slots; i += 512) {                   // [32 d][lane]
-      const int l = i & 63, d = 32 * (i >> 6) + (l & 15), r = 4 * (l >> 4);
-      uint32_t o[4];
+    // Four neighbouring lanes hold 16 d of four tokens.  Each takes four of the d from all of them (their dwords first, one lane after the
+    // other), and then turns the 4 x 4 bytes over: a dword is four tokens of one d.
+    auto give = [&](int j) {                                 // what lane ^ j takes
+      const int want = (lane ^ j) & 3;
+      return (int)(want == 0 ? o[0] : want == 1 ? o[1] : want == 2 ? o[2] : o[3]);
+    };
+    const uint32_t g[4] = {(uint32_t)give(0), (uint32_t)__builtin_amdgcn_update_dpp(0, give(1), 0xb1, 0xf, 0xf, true),
+                           (uint32_t)__builtin_amdgcn_update_dpp(0, give(2), 0x4e, 0xf, 0xf, true),
+                           (uint32_t)__builtin_amdgcn_update_dpp(0, give(3), 0x1b, 0xf, 0xf, true)};
+    uint32_t a[4];                                           // by token: g[j] came from lane ^ j
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int8_t* q = code + (r + 16 * (k & 1)) * ld + d + 16 * (k >> 1);
-        o[k] = (uint32_t)(uint8_t)q[0] | (uint32_t)(uint8_t)q[ld] << 8 | (uint32_t)(uint8_t)q[2 * ld] << 16 | (uint32_t)(uint8_t)q[3 * ld] << 24;
-      }
-      *reinterpret_cast<uint4*>(out + (size_t)i * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+    for (int r = 0; r < 4; ++r) {
+      const int j = (lane ^ r) & 3;
+      a[r] = j == 0 ? g[0] : j == 1 ? g[1] : j == 2 ? g[2] : g[3];
+    }
+    const uint32_t p01 = __builtin_amdgcn_perm(a[1], a[0], 0x05010400), q01 = __builtin_amdgcn_perm(a[1], a[0], 0x07030602);   // d 0 1 and 2 3 of tokens 0, 1
+    const uint32_t p23 = __builtin_amdgcn_perm(a[3], a[2], 0x05010400), q23 = __builtin_amdgcn_perm(a[3], a[2], 0x07030602);
+    const uint32_t by[4] = {__builtin_amdgcn_perm(p23, p01, 0x05040100), __builtin_amdgcn_perm(p23, p01, 0x07060302),
+                            __builtin_amdgcn_perm(q23, q01, 0x05040100), __builtin_amdgcn_perm(q23, q01, 0x07060302)};
+    if (i < slots) {
+      const int d = 64 * (i >> 7) + 16 * (i >> 4 & 3) + 4 * (lane & 3);
+      uint32_t* const to = reinterpret_cast<uint32_t*>(code) + ((d >> 5) * 64 + 16 * (i >> 2 & 3) + (d & 15)) * 4 + 2 * (d >> 4 & 1) + (i >> 6 & 1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to[4 * e] = by[e];
     }
   }
+  if (!is_v) return;
+  __syncthreads();
+  for (int i = t; i < slots; i += 512) reinterpret_cast<uint4*>(out)[i] = code[i];
 }
 void launch_cache_fill(int prec, const CacheSource& src, const int32_t* lengths, int tokens, const CacheShape& s, void* cache, hipStream_t st) {
   const size_t es = prec ? 2 : 4;
@@ -185,14 +192,14 @@ __device__ __forceinline__ void cache_operand(uint32_t a, uint32_t b, Frag<bf16_
   f.v = make_uint4(two(a, 0), two(a, 16), two(b, 0), two(b, 16));
 }
 
-constexpr int ATTEND_WAVES = 8, ATTEND_CHUNK = 128, ATTEND_LD = ATTEND_CHUNK + 4;
+constexpr int ATTEND_WAVES = 8, ATTEND_CHUNK = 128, ATTEND_LD = ATTEND_CHUNK + 4, ATTEND_SPLITS = 512;
 struct AttendPlan { int g_tiles, splits; };                 // tiles of 16 queries; ranges of the tokens
 static AttendPlan attend_plan(const CacheShape& s, int per, int q_heads, int tokens) {
   AttendPlan p;
   p.g_tiles = (per * (q_heads / s.heads) + 15) / 16;
   const long units = (long)s.seqs * s.heads * p.g_tiles;
   const int chunks = std::max(1, (tokens + ATTEND_CHUNK - 1) / ATTEND_CHUNK);
-  p.splits = (int)std::min<long>(chunks, std::max<long>(1, 512 / units));
+  p.splits = (int)std::min<long>(std::min(chunks, ATTEND_SPLITS), std::max<long>(1, 512 / units));
   return p;
 }
 size_t cache_attend_workspace(const CacheShape& s, int per, int q_heads, int tokens) {
@@ -239,19 +246,24 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
 #pragma unroll
   for (int e = 0; e < EPW; ++e) acc[e][0] = acc[e][1] = v4f{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;                              // of query t / 32, in its 32 threads
-  // keys are asked for a chunk ahead, values before the chunk's scores are made: both are on their way in every phase
+  // keys are asked for a chunk ahead, values before the chunk's scores are made: both are on their way in every phase.  Without ranges the
+  // first of them do not wait for the sequence's length: what lies behind it is there, and not used.
+  // Few tokens leave wavefronts without a tile: `parts` of them then share one, each some of its d.
+  const int bound = a.splits == 1 ? a.tokens : last;
+  const int parts = a.splits > 1 || a.tokens > 64 ? 1 : a.tokens > 32 ? 2 : a.tokens > 16 ? 4 : 8, tiles = 8 / parts;
+  const int share = (chunks + parts - 1) / parts, ch0 = w / tiles * share, nch = min(share, chunks - ch0), my_tile = 16 * (w % tiles);
   uint4 kr[4 * EPW], vr[4][EPW];
   float ks = 0.f;
   auto fetch_keys = [&](int t0) {
-    const int tile = t0 + 16 * w;
-    if (tile >= last) return;
-    const uint4* kp = reinterpret_cast<const uint4*>(kc + (size_t)(tile >> 4) * chunks * 1024) + lane;
+    const int tile = t0 + my_tile;
+    if (tile >= bound) return;
+    const uint4* kp = reinterpret_cast<const uint4*>(kc + ((size_t)(tile >> 4) * chunks + ch0) * 1024) + lane;
 #pragma unroll
-    for (int ch = 0; ch < 4 * EPW; ++ch) if (ch < chunks) kr[ch] = kp[ch * 64];
+    for (int ch = 0; ch < 4 * EPW; ++ch) if (ch < nch) kr[ch] = kp[ch * 64];
     ks = c.kscale[at + (tile >> 5)];
   };
   fetch_keys(first);
-  if (first < last)
+  if (first < bound)
     for (int i = t; i < chunks * 128; i += 64 * ATTEND_WAVES) {   // the queries as operands: [chunk][half][part][lane]
       const int l = i & 63, ch = i >> 7, h = i >> 6 & 1, d = 64 * ch + 16 * (l >> 4) + 8 * h;
       Frag<bf16_t> f[QP];
@@ -263,27 +275,28 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
   __syncthreads();
   for (int t0 = first; t0 < last; t0 += ATTEND_CHUNK) {
     const int tok = t0 + 4 * (t & 31);
-    const float vs = tok < last ? c.vscale[at + (tok >> 5)] : 0.f;
+    const float vs = tok < bound ? c.vscale[at + (tok >> 5)] : 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int blk = my_ts + i * ts;
-      if (blk >= ATTEND_CHUNK / CACHE_BLOCK || t0 + blk * CACHE_BLOCK >= last) break;
+      if (blk >= ATTEND_CHUNK / CACHE_BLOCK || t0 + blk * CACHE_BLOCK >= bound) break;
       const uint4* vp = reinterpret_cast<const uint4*>(vc + (size_t)((t0 >> 5) + blk) * chunks * 2048) + lane;
 #pragma unroll
       for (int e = 0; e < EPW; ++e) if (mine + e < E) vr[i][e] = vp[(mine + e) * 64];
     }
-    if (t0 + 16 * w < last) {
+    if (t0 + my_tile < last) {
       v4f z[2] = {v4f{0.f, 0.f, 0.f, 0.f}, v4f{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
       for (int ch = 0; ch < 4 * EPW; ++ch)
-        if (ch < chunks) {
+        if (ch < nch) {
           Frag<bf16_t> k0, k1, qf;
+          const uint4* const qp = s_q + (size_t)(ch0 + ch) * 2 * QP * 64 + lane;
           cache_operand(kr[ch].x, kr[ch].y, k0);
           cache_operand(kr[ch].z, kr[ch].w, k1);
 #pragma unroll
           for (int p = QP - 1; p >= 0; --p) {
-            qf.v = s_q[(ch * 2 * QP + p) * 64 + lane]; mma16(z[0], k0, qf);
-            qf.v = s_q[((ch * 2 + 1) * QP + p) * 64 + lane]; mma16(z[1], k1, qf);
+            qf.v = qp[p * 64]; mma16(z[0], k0, qf);
+            qf.v = qp[(QP + p) * 64]; mma16(z[1], k1, qf);
           }
         }
       const float sc = ks * a.scale;
@@ -294,12 +307,15 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
     __syncthreads();
     {
       const int i = t >> 5, j = t & 31;
-      const float4 x4 = *reinterpret_cast<const float4*>(s_s + i * ATTEND_LD + 4 * j);
-      float x[4] = {x4.x, x4.y, x4.z, x4.w}, mx = -INFINITY;
+      float x[4] = {0.f, 0.f, 0.f, 0.f}, mx = -INFINITY;
+      if (j < 4 * tiles)
+        for (int p = 0; p < parts; ++p) {
+          const float4 x4 = *reinterpret_cast<const float4*>(s_s + i * ATTEND_LD + 16 * tiles * p + 4 * j);
+          x[0] += x4.x; x[1] += x4.y; x[2] += x4.z; x[3] += x4.w;
+        }
 #pragma unroll
       for (int e = 0; e < 4; ++e) if (tok + e < last) mx = fmaxf(mx, x[e]);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+      mx = half_max(mx);
       const float mn = fmaxf(m, mx), ms = mn > -INFINITY ? mn : 0.f;
       const float f = m > -INFINITY ? (FAST ? __expf(m - ms) : expf(m - ms)) : 0.f;
       float sum = 0.f;
@@ -309,8 +325,7 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
         sum += x[e];
         x[e] = tok + e < last ? x[e] * vs : 0.f;
       }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      sum = half_sum(sum);
       l = l * f + sum;
       m = mn;
       if (j == 0) s_f[i] = f;
@@ -378,7 +393,7 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
   if (a.splits > 1) {
     const size_t slot = (size_t)unit * a.splits + split;
     if (t < 16) { a.ml[(slot * 16 + t) * 2] = s_m[t]; a.ml[(slot * 16 + t) * 2 + 1] = s_l[t]; }
-    if (first >= last) return;
+    if (first >= last || g0 + g >= G) return;
     float* part = a.part + (slot * 16 + g) * chunks * 64;
 #pragma unroll
     for (int e = 0; e < EPW; ++e)
@@ -403,7 +418,6 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
       }
 }
 // joins the ranges of a query: one workgroup each, its threads a column of four and a share of the ranges
-constexpr int ATTEND_SPLITS = 512;
 template <typename T>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a, CacheShape s) {
   __shared__ float s_w[ATTEND_SPLITS];

@@ -84,6 +84,23 @@ struct ReorderJobs { ReorderJob job[REORDER_MAX]; };
 void launch_search_reorder(const ReorderJobs& jobs, int n, const int32_t* rows, int count, int src_rows, hipStream_t st);
 
 // ---- shared ------------------------------------------------------------------------------------------
+// Over the 16 lanes of a row, in every lane, by DPP moves (a shuffle through LDS is ten times as long).
+#define CMT_ROW16(v, op)                                                                                                        \
+  do {                                                                                                                          \
+    v = op(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, true)));  /* quad_perm 1 0 3 2 */ \
+    v = op(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, true)));  /* quad_perm 2 3 0 1 */ \
+    v = op(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true))); /* row_half_mirror */   \
+    v = op(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, true))); /* row_mirror */        \
+  } while (0)
+__device__ __forceinline__ float add_of(float a, float b) { return a + b; }
+__device__ __forceinline__ float row16_max(float v) { CMT_ROW16(v, fmaxf); return v; }
+__device__ __forceinline__ float row16_sum(float v) { CMT_ROW16(v, add_of); return v; }
+#undef CMT_ROW16
+__device__ __forceinline__ float half_max(float v) { v = row16_max(v); return fmaxf(v, __shfl_xor(v, 16, 64)); }   // over 32 lanes
+__device__ __forceinline__ float half_sum(float v) { v = row16_sum(v); return v + __shfl_xor(v, 16, 64); }
+__device__ __forceinline__ float lanes_max(float v) { v = half_max(v); return fmaxf(v, __shfl_xor(v, 32, 64)); }   // over all 64
+__device__ __forceinline__ float lanes_sum(float v) { v = half_sum(v); return v + __shfl_xor(v, 32, 64); }
+
 // An fp32 number as three bf16 that add up to it, cut off rather than rounded (8 + 8 + 8 bits; none can overflow).  Infinities and NaN
 // stand in the first part alone.
 struct Parts3 { uint32_t h, m, l; };                       // bits as of an fp32, lower half 0

@@ -14,15 +14,6 @@ __device__ __forceinline__ unsigned search_sortable(float v) {   // larger numbe
   const unsigned u = __float_as_uint(v + 0.f);
   return u ^ ((int)u < 0 ? 0xffffffffu : 0x80000000u);
 }
-__device__ __forceinline__ float search_wave_max(float v) {
-#define STEP(ctrl, rows) v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), ctrl, rows, 0xf, false)))
-  STEP(0x111, 0xf); STEP(0x112, 0xf); STEP(0x114, 0xf); STEP(0x118, 0xf);
-  STEP(0x142, 0xa);
-  STEP(0x143, 0xc);
-#undef STEP
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
-
 // ---- statistics of the groups ---------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void search_groups_kernel(const T* __restrict__ logits, size_t ld, const float* __restrict__ scores, int rows, int V,
@@ -51,12 +42,12 @@ __global__ __launch_bounds__(256) void search_groups_kernel(const T* __restrict_
   float mx = x[0];
 #pragma unroll
   for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[i]);          // (a NaN is never the largest, but is in the sum)
-  mx = search_wave_max(mx);
+  mx = lanes_max(mx);
   const float ms = mx > -INFINITY ? mx : 0.f;
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) sum += expf(x[i] - ms);
-  sum = wave_sum(sum);
+  sum = lanes_sum(sum);
   if (lane == 0) stat[id] = make_float2(mx, sum);
 }
 
@@ -148,13 +139,14 @@ __global__ __launch_bounds__(SELECT_NT) void search_select_kernel(const T* __res
     double base = -INFINITY;
     if (c > -INFINITY) {
       const float2* p = stat + (size_t)(row0 + s) * groups;
-      float mx = -INFINITY;
-      for (int g = lane; g < groups; g += 64) mx = fmaxf(mx, p[g].x);
-      mx = search_wave_max(mx);
-      float sum = 0.f;
+      const float2 x0 = lane < groups ? p[lane] : make_float2(-INFINITY, 0.f);
+      float mx = x0.x;
+      for (int g = lane + 64; g < groups; g += 64) mx = fmaxf(mx, p[g].x);
+      mx = lanes_max(mx);
       const float ms = mx > -INFINITY ? mx : 0.f;
-      for (int g = lane; g < groups; g += 64) { const float2 x = p[g]; sum += x.x > -INFINITY ? x.y * expf(x.x - ms) : x.y; }
-      sum = wave_sum(sum);
+      float sum = x0.x > -INFINITY ? x0.y * expf(x0.x - ms) : x0.y;
+      for (int g = lane + 64; g < groups; g += 64) { const float2 x = p[g]; sum += x.x > -INFINITY ? x.y * expf(x.x - ms) : x.y; }
+      sum = lanes_sum(sum);
       // (no finite logit, an infinite one or one that is no number: no extension of this row)
       if (c < INFINITY && mx > -INFINITY && mx < INFINITY && sum < INFINITY) base = (double)c - (double)mx - (double)logf(sum);
     }
@@ -185,7 +177,7 @@ __global__ __launch_bounds__(SELECT_NT) void search_select_kernel(const T* __res
   if (t < tops) s_top[t] = sh.wi[t];
   const float floor_ = tops == n ? (float)sh.wv[n - 1] : -INFINITY;
   __syncthreads();
-  const int found = select_best(sh, n, tops * SEARCH_GROUP, floor_, [&](int i, unsigned& index) {
+  const int found = tops == 0 ? 0 : select_best(sh, n, tops * SEARCH_GROUP, floor_, [&](int i, unsigned& index) {
     const int id = s_top[i / SEARCH_GROUP], s = id / groups, v = (id - s * groups) * SEARCH_GROUP + i % SEARCH_GROUP;
     index = (unsigned)s * (unsigned)V + (unsigned)v;
     if (v >= V) return -(double)INFINITY;
