@@ -321,6 +321,19 @@ int cmt_beam_select(const void* logits_dev, int32_t type, int64_t pitch, const f
  * returns).  A row whose number is outside [0, source_rows) is left as it was.  No target may overlap a source or another target. */
 typedef struct cmt_reorder_tensor { const void* source_dev; void* target_dev; int64_t source_pitch, target_pitch, row_bytes; } cmt_reorder_tensor;
 int cmt_beam_reorder(const int32_t* rows_dev, int32_t count, int32_t source_rows, const cmt_reorder_tensor* tensors, int32_t n, void* hip_stream);
+/* The decoder of a handle in small numbers: cmt_beam_decode with the weights of the decoder's layers, of W_c and of the output layer in
+ * 4 bits (a fifth of the 16-bit ones' bytes, with groups of 64) and the source rows (keys W_a^T H_s and states H_s) in 8.  Biases, embeddings, the encoder, states, cells and scores are as in
+ * cmt_beam_decode, and so are the arguments, the search's rules and the errors.
+ *   cmt_quant_decoder_bytes  of the packed weights and of the workspace of a search (any B, S and beam that the configuration allows);
+ *   cmt_quant_decoder_pack   writes the packed weights from the handle's parameters as they are (enqueued; again after they change);
+ *   cmt_quant_beam_decode    one search; beam 1 and length_penalty 0 is greedy decoding.  Synchronises the stream.  The handle's workspace is
+ *                            used as by cmt_beam_decode; the packed weights are read only and may be shared by handles of one configuration.
+ * Weights and workspace are the caller's, 256-byte aligned; group 32, 64 or 128 as in cmt_quant_weight_bytes. */
+int cmt_quant_decoder_bytes(const cmt_config* cfg, int32_t group, size_t* weight_bytes, size_t* workspace_bytes);
+int cmt_quant_decoder_pack(cmt_handle* h, int32_t group, void* weights_dev);
+int cmt_quant_beam_decode(cmt_handle* h, int32_t group, const void* weights_dev, void* workspace_dev, const int32_t* src_ids_dev,
+                          const int32_t* src_len_dev, int32_t B, int32_t S, int32_t max_len, int32_t beam, float length_penalty, int32_t eos_id,
+                          int32_t* out_ids_dev, int32_t* out_len_dev, float* out_score_dev);
 
 #ifdef __cplusplus
 }

@@ -22,6 +22,7 @@ EXPORTS = [
     "cmt_operator_error", "cmt_quant_weight_bytes", "cmt_quant_weight_pack", "cmt_quant_weight_encode",
     "cmt_quant_weight_values", "cmt_quant_product", "cmt_cache_bytes", "cmt_cache_fill", "cmt_cache_read",
     "cmt_cache_attend_workspace", "cmt_cache_attend", "cmt_beam_select_workspace", "cmt_beam_select", "cmt_beam_reorder",
+    "cmt_quant_decoder_bytes", "cmt_quant_decoder_pack", "cmt_quant_beam_decode",
 ]
 
 
@@ -106,6 +107,9 @@ def load_library():
     lib.cmt_beam_select_workspace.argtypes = [i32, i32, i32, szp]
     lib.cmt_beam_select.argtypes = [vp, i32, i64, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.cmt_beam_reorder.argtypes = [vp, i32, i32, vp, i32, vp]            # (an array of CmtReorderTensor)
+    lib.cmt_quant_decoder_bytes.argtypes = [cfgp, i32, szp, szp]
+    lib.cmt_quant_decoder_pack.argtypes = [vp, i32, vp]
+    lib.cmt_quant_beam_decode.argtypes = [vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, C.c_float, i32, vp, vp, vp]
     for name in EXPORTS:
         if name not in ("cmt_destroy", "cmt_last_error", "cmt_operator_error"):
             getattr(lib, name).restype = C.c_int

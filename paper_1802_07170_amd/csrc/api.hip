@@ -26,6 +26,7 @@
 
 #include "../../include/cytonmt_hip.h"
 #include "kernels.h"
+#include "lowbit.h"
 #include "recur_plan.h"
 #include "row_pitch.h"
 #include "section_gate.h"
@@ -1829,6 +1830,173 @@ int cmt_beam_decode(cmt_handle* h, const int32_t* src_ids_dev, const int32_t* sr
   hipError_t e = hipStreamSynchronize(st);
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(h, e, "cmt_beam_decode");
+  const int flags = *h->h_flags;
+  if (flags & 3) return fail(h, CMT_ERANGE, (flags & 1) ? "a token id is outside its vocabulary" : "a length is outside [1, padded length]");
+  return CMT_OK;
+}
+
+// ---- the decoder in small numbers -----------------------------------------------------------------------
+namespace {
+// The packed weights of a decoder behind each other: its layers, W_c, W_o.
+struct QuantDecoder {
+  std::vector<QuantShape> shape;
+  std::vector<size_t> at;
+  size_t bytes = 0;
+  QuantDecoder(const cmt_config& c, int group) {
+    const int E = c.emb_dim, H = c.hidden;
+    for (int l = 0; l < c.layers; ++l) add(4 * H, l ? 2 * H : E + 2 * H, group);
+    add(H, 2 * H, group);
+    add(c.tgt_vocab, H, group);
+  }
+  QuantWeightRef weight(int i, const void* base) const { return QuantWeightRef{shape[i], (const char*)base + at[i]}; }
+ private:
+  void add(int n, int k, int group) {
+    shape.push_back(QuantShape{n, k, group});
+    at.push_back(bytes);
+    bytes += shape.back().bytes();
+  }
+};
+// What one search keeps beside the handle's workspace, for R rows: the operands [embedding; H_o; h] and [input; h] of the layers and
+// [C_s; H_t] of the attentional layer, states and H_o that a position makes (the choice of hypotheses moves them to where the next one
+// reads them), gates, logits, the source rows in 8 bits.
+struct QuantSearch {
+  char* xcat = nullptr; char* xl[8] = {}; char* xc = nullptr; char* hn[8] = {}; char* ho = nullptr;
+  float* c[8] = {}; float* cn[8] = {}; float* gates = nullptr; float* logits = nullptr;
+  void* cache = nullptr; void* attend = nullptr; void* stats = nullptr;
+  size_t bytes = 0;
+  // attend_bytes: of the attention's workspace
+  QuantSearch(const cmt_config& cf, char* base, int R, int B, int S, size_t attend_bytes) {
+    const size_t E = cf.emb_dim, H = cf.hidden, es = cf.precision ? 2 : 4;
+    Bump a(base);
+    xcat = a.take(R * (E + 2 * H) * es);
+    xc = a.take(R * 2 * H * es);
+    ho = a.take(R * H * es);
+    for (int l = 0; l < cf.layers; ++l) {
+      if (l) xl[l] = a.take(R * 2 * H * es);
+      hn[l] = a.take(R * H * es);
+      c[l] = (float*)a.take(R * H * 4);
+      cn[l] = (float*)a.take(R * H * 4);
+    }
+    gates = (float*)a.take(R * 4 * H * 4);
+    logits = (float*)a.take((size_t)R * cf.tgt_vocab * 4);
+    stats = a.take(search_workspace(R, 1, cf.tgt_vocab));
+    cache = a.take(CacheShape{B, 1, cf.hidden, S}.bytes());
+    attend = a.take(attend_bytes);
+    bytes = (a.off + 255) & ~(size_t)255;
+  }
+};
+bool quant_group_ok(int group) { return group == 32 || group == 64 || group == 128; }
+}  // namespace
+
+int cmt_quant_decoder_bytes(const cmt_config* cfg, int32_t group, size_t* weight_bytes, size_t* workspace_bytes) {
+  if (!config_ok(cfg, nullptr) || !quant_group_ok(group)) return CMT_EINVAL;
+  if (weight_bytes) *weight_bytes = QuantDecoder(*cfg, group).bytes;
+  if (workspace_bytes) {
+    size_t attend = 0;                               // (the number of ranges depends on how many sentences there are)
+    for (int b = 1; b <= cfg->max_batch; ++b) attend = std::max(attend, cache_attend_workspace(CacheShape{b, 1, cfg->hidden, cfg->max_src_len}, 1, 1, cfg->max_src_len));
+    *workspace_bytes = QuantSearch(*cfg, nullptr, cfg->max_batch, cfg->max_batch, cfg->max_src_len, attend).bytes;
+  }
+  return CMT_OK;
+}
+
+int cmt_quant_decoder_pack(cmt_handle* h, int32_t group, void* weights_dev) {
+  if (!h) return CMT_EINVAL;
+  if (!weights_dev || ((uintptr_t)weights_dev & 255)) return fail(h, CMT_EINVAL, "weights must be a 256-byte aligned device pointer");
+  if (!quant_group_ok(group)) return fail(h, CMT_EINVAL, "group must be 32, 64 or 128");
+  const QuantDecoder q(h->cfg, group);
+  const int L = h->cfg.layers;
+  for (int i = 0; i < L + 2; ++i) {
+    const size_t off = i < L ? h->dec[i].w_off : i == L ? h->off_Wc : h->off_Wo;
+    launch_quant_pack(0, h->params + off, (size_t)q.shape[i].K, q.shape[i], (char*)weights_dev + q.at[i], h->st);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(h, e, "cmt_quant_decoder_pack");
+  return CMT_OK;
+}
+
+int cmt_quant_beam_decode(cmt_handle* h, int32_t group, const void* weights_dev, void* workspace_dev, const int32_t* src_ids_dev,
+                          const int32_t* src_len_dev, int32_t B, int32_t S, int32_t max_len, int32_t beam, float length_penalty, int32_t eos_id,
+                          int32_t* out_ids_dev, int32_t* out_len_dev, float* out_score_dev) {
+  if (!h) return CMT_EINVAL;
+  const cmt_config& c = h->cfg;
+  if (!weights_dev || !workspace_dev || ((uintptr_t)weights_dev & 255) || ((uintptr_t)workspace_dev & 255))
+    return fail(h, CMT_EINVAL, "weights and workspace must be 256-byte aligned device pointers");
+  if (!quant_group_ok(group)) return fail(h, CMT_EINVAL, "group must be 32, 64 or 128");
+  if (!src_ids_dev || !src_len_dev || !out_ids_dev || !out_len_dev || !out_score_dev) return fail(h, CMT_EINVAL, "null pointer");
+  if (B < 1 || S < 1 || S > c.max_src_len || max_len < 1 || max_len > c.max_tgt_len)
+    return fail(h, CMT_EINVAL, "B, S or max_len outside [1, configured maximum]");
+  if (beam < 1 || beam > 16) return fail(h, CMT_EINVAL, "beam must be in [1, 16]");
+  if ((long long)B * beam > c.max_batch) return fail(h, CMT_EINVAL, "B * beam exceeds max_batch (one decoder row per hypothesis)");
+  if (!(length_penalty >= 0.f) || !isfinite(length_penalty)) return fail(h, CMT_EINVAL, "length_penalty must be finite and >= 0");
+  if (eos_id < 0 || eos_id >= c.tgt_vocab) return fail(h, CMT_EINVAL, "eos_id outside the target vocabulary");
+  const int p = h->prec, E = c.emb_dim, H = c.hidden, L = c.layers, V = c.tgt_vocab, K = beam, R = B * K;
+  const int BpE = round_up(B, 16);
+  const size_t esz = h->esz;
+  hipStream_t st = h->st;
+  h->B = B; h->Bp = BpE; h->S = S; h->T = max_len;
+  h->have_step = false;
+  h->phase_n = 0;
+  const float keep_p = h->drop_p;
+  h->drop_p = 0.f;                                   // inference: no dropout
+  launch_fill_f32((float*)h->flags, 1, 0.f, st);
+  const GatherSide side{h->Pw(h->off_Esrc), c.src_vocab, src_ids_dev, src_len_dev, S, 0, 0, h->Xs, h->mask_s, h->tok_s, nullptr, h->len_s};
+  launch_gather(p, &side, 1, E, B, BpE, h->flags, st);
+  const char* Hs; int ldHs;
+  note_capture(h);
+  Section sec(h);
+  sec.open(false);
+  enqueue_encoder(h, S, &Hs, &ldHs, false, false, nullptr);
+  sec.close();
+  h->drop_p = keep_p;
+  const QuantDecoder q(c, group);
+  const CacheShape shape{B, 1, H, S};
+  const QuantSearch s(c, (char*)workspace_dev, R, B, S, cache_attend_workspace(shape, K, 1, S));
+  // source rows are time-major: position t of sentence b at row t * BpE + b
+  const CacheSource src{h->Kmat, Hs, (size_t)H, (size_t)BpE * H, 0, (size_t)ldHs, (size_t)BpE * ldHs, 0};
+  launch_cache_fill(p, src, h->len_s, S, shape, s.cache, st);
+  BeamState& bs = h->beam;
+  bs.hist_ld = round_up(R, 16);
+  launch_beam_init(bs, B, bs.hist_ld, K, c.bos_id, st);
+  const size_t X0 = E + 2 * H, X = 2 * H;            // widths of the operands
+  char* h_in[8] = {};                                // where a layer reads its state
+  for (int l = 0; l < L; ++l) h_in[l] = l ? s.xl[l] + H * esz : s.xcat + (E + H) * esz;
+  launch_fill_T(p, s.xcat, (size_t)R * X0, st);      // H_o^{<-1>} = 0
+  for (int l = 0; l < L; ++l) {                      // one decoder row per hypothesis: the initial states repeated
+    launch_beam_expand((int)esz, h->dec[l].Hst, h->dec[l].ph, h_in[l], (int)(l ? X : X0), R, R, K, H, st);
+    launch_beam_expand(4, h->dec[l].Cst, H, s.c[l], H, R, R, K, H, st);
+  }
+  auto job = [](const void* from, size_t from_pitch, void* to, size_t to_pitch, size_t bytes) {
+    return ReorderJob{(const char*)from, (char*)to, from_pitch, to_pitch, (int)bytes, 16};
+  };
+  ReorderJobs embed{}, follow{};
+  embed.job[0] = job(h->Pw(h->off_Etgt), E * esz, s.xcat, X0 * esz, E * esz);
+  int n = 0;
+  follow.job[n++] = job(s.ho, H * esz, s.xcat + E * esz, X0 * esz, H * esz);
+  for (int l = 0; l < L; ++l) {
+    follow.job[n++] = job(s.hn[l], H * esz, h_in[l], (l ? X : X0) * esz, H * esz);
+    follow.job[n++] = job(s.cn[l], (size_t)H * 4, s.c[l], (size_t)H * 4, (size_t)H * 4);
+  }
+  SearchAdvance adv{bs.hist_tok, bs.hist_par, bs.fin_step, bs.fin_par, bs.fin_tok, bs.fin_score, bs.hist_ld, 0, max_len, eos_id, length_penalty};
+  for (int j = 0; j < max_len; ++j) {
+    launch_search_reorder(embed, 1, bs.tok, R, V, st);
+    for (int l = 0; l < L; ++l) {
+      launch_quant_product(p, l ? s.xl[l] : s.xcat, l ? X : X0, q.weight(l, weights_dev), R, h->params + h->dec[l].b_off, false, 0, s.gates, 4 * (size_t)H, st);
+      // the state goes to where the position's next layer (the last one's: the attentional layer) reads it
+      launch_quant_cell(p, s.gates, s.c[l], s.cn[l], s.hn[l], H, l + 1 < L ? s.xl[l + 1] : s.xc + H * esz, X, R, H, st);
+    }
+    launch_cache_attend(p, shape, s.cache, s.hn[L - 1], H, K, 1, S, 1.f, s.xc, X, s.attend, st);
+    launch_quant_product(p, s.xc, X, q.weight(L, weights_dev), R, nullptr, true, p, s.ho, H, st);
+    launch_quant_product(p, s.ho, H, q.weight(L + 1, weights_dev), R, h->params + h->off_Bo, false, 0, s.logits, V, st);
+    adv.j = j;
+    launch_search_select(0, s.logits, V, bs.cum, B, K, V, K, bs.new_cum, bs.parent, bs.tok, &adv, s.stats, st);
+    std::swap(bs.cum, bs.new_cum);                   // (both hold what one search needs: which is which does not matter afterwards)
+    if (j + 1 < max_len) launch_search_reorder(follow, n, bs.parent, R, R, st);
+  }
+  launch_beam_finish(bs, B, K, max_len, c.pad_id, out_ids_dev, out_len_dev, out_score_dev, st);
+  (void)hipMemcpyAsync(h->h_flags, h->flags, sizeof(int), hipMemcpyDeviceToHost, st);
+  hipError_t e = hipStreamSynchronize(st);
+  if (e == hipSuccess) e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(h, e, "cmt_quant_beam_decode");
   const int flags = *h->h_flags;
   if (flags & 3) return fail(h, CMT_ERANGE, (flags & 1) ? "a token id is outside its vocabulary" : "a length is outside [1, padded length]");
   return CMT_OK;

@@ -29,6 +29,9 @@ void launch_quant_values(const void* packed, const QuantShape& q, float* out, hi
 // y [M, N] = f(x [M, K] W^T + bias), f = tanh or nothing; x of type prec, y of type y_prec; bias fp32 or null.
 void launch_quant_product(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, bool tanh, int y_prec, void* y,
                           size_t ldy, hipStream_t st);
+// The cell of an LSTM step: gates [R, 4 H] fp32 (blocks i, f, g, o, before their nonlinearities), c_prev [R, H] -> c [R, H] fp32 and the state
+// in type prec to two places (h2 may be null; pitches in elements).  H and the pitches are multiples of 4, as are the addresses in elements.
+void launch_quant_cell(int prec, const float* gates, const float* c_prev, float* c, void* h, size_t ldh, void* h2, size_t ldh2, int R, int H, hipStream_t st);
 
 // ---- cache.hip: source rows in 8 bits -------------------------------------------------------------
 // Per (sequence, head, block of 32 tokens) one fp32 scale for the keys and one for the values; codes are whole numbers -127..127.
@@ -72,7 +75,7 @@ constexpr int SEARCH_MAX_VOCAB = 1 << 26;
 // What a search that is kept on the device does with the best extensions (the rules of cmt_beam_decode): those that end leave the
 // beam, the others fill its places, best first.  Rows beyond R and lists as in BeamState.
 struct SearchAdvance {
-  int32_t *hist_tok, *hist_par, *nlive, *fin_step, *fin_par, *fin_tok; float* fin_score;
+  int32_t *hist_tok, *hist_par, *fin_step, *fin_par, *fin_tok; float* fin_score;
   int hist_ld, j, max_len, eos; float alpha;
 };
 size_t search_workspace(int B, int K, int V);

@@ -426,4 +426,35 @@ void launch_quant_product(int prec, const void* x, size_t ldx, const QuantWeight
   if (prec) go(bf16_t{}); else go(float{});
 }
 
+// ---- the cell behind a layer's product ----------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void quant_cell_kernel(const float* __restrict__ gates, const float* __restrict__ c_prev, float* __restrict__ c,
+                                                         T* __restrict__ h, size_t ldh, T* __restrict__ h2, size_t ldh2, int R, int H) {
+  constexpr bool FAST = sizeof(T) == 2;
+  const int per = H >> 2, i = blockIdx.x * 256 + threadIdx.x, r = i / per, u = (i - r * per) * 4;
+  if (r >= R) return;
+  const float* g = gates + (size_t)r * 4 * H + u;
+  const float4 gi = *reinterpret_cast<const float4*>(g), gf = *reinterpret_cast<const float4*>(g + H);
+  const float4 gg = *reinterpret_cast<const float4*>(g + 2 * H), go = *reinterpret_cast<const float4*>(g + 3 * H);
+  const float4 cp = *reinterpret_cast<const float4*>(c_prev + (size_t)r * H + u);
+  float4 cn;
+  T hn[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = sigm_of<FAST>((&gf.x)[e]) * (&cp.x)[e] + sigm_of<FAST>((&gi.x)[e]) * tanh_of<FAST>((&gg.x)[e]);
+    (&cn.x)[e] = x;
+    hn[e] = from_f<T>(sigm_of<FAST>((&go.x)[e]) * tanh_of<FAST>(x));
+  }
+  *reinterpret_cast<float4*>(c + (size_t)r * H + u) = cn;
+  struct alignas(4 * sizeof(T)) Four { T v[4]; };
+  const Four f{{hn[0], hn[1], hn[2], hn[3]}};
+  *reinterpret_cast<Four*>(h + r * ldh + u) = f;
+  if (h2) *reinterpret_cast<Four*>(h2 + r * ldh2 + u) = f;
+}
+void launch_quant_cell(int prec, const float* gates, const float* c_prev, float* c, void* h, size_t ldh, void* h2, size_t ldh2, int R, int H, hipStream_t st) {
+  const dim3 grid((unsigned)(((size_t)R * (H / 4) + 255) / 256));
+  if (prec) hipLaunchKernelGGL(quant_cell_kernel<bf16_t>, grid, dim3(256), 0, st, gates, c_prev, c, (bf16_t*)h, ldh, (bf16_t*)h2, ldh2, R, H);
+  else hipLaunchKernelGGL(quant_cell_kernel<float>, grid, dim3(256), 0, st, gates, c_prev, c, (float*)h, ldh, (float*)h2, ldh2, R, H);
+}
+
 }  // namespace cmt

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 
+import numpy as np
 import torch
 
 from . import binding
@@ -281,3 +282,40 @@ def _row_pitch(t, i):
             raise ValueError(f"tensors {i}: the elements of a row must lie side by side")
         side *= t.shape[d]
     return t.stride(0) if t.shape[0] > 1 else side
+
+
+class QuantDecoder:
+    """A trainer's decoder in small numbers: its weights, W_c and the output layer in 4 bits, the source rows in 8.  The weights are those that the
+    trainer has when this is made; `pack` renews them."""
+
+    def __init__(self, trainer, group=64):
+        weights, workspace = C.c_size_t(), C.c_size_t()
+        if trainer.lib.cmt_quant_decoder_bytes(C.byref(trainer.ccfg), group, C.byref(weights), C.byref(workspace)) != CMT_OK:
+            raise CmtError(binding.CMT_EINVAL, "group must be 32, 64 or 128")
+        self.trainer, self.group = trainer, group
+        with torch.cuda.stream(trainer.stream):
+            self.weights = torch.empty(weights.value, dtype=torch.uint8, device=trainer.device)
+            self.workspace = torch.empty(workspace.value, dtype=torch.uint8, device=trainer.device)
+        self.pack()
+
+    def pack(self):
+        """Writes the packed weights from the trainer's parameters."""
+        tr = self.trainer
+        tr._check(tr.lib.cmt_quant_decoder_pack(tr.h, self.group, self.weights.data_ptr()))
+
+    def beam_decode(self, src_ids, src_len, max_len, beam=10, length_penalty=0.6, eos_id=3):
+        """As Trainer.beam_decode: ids [B, max_len], lengths [B], normalised scores [B] (numpy)."""
+        tr = self.trainer
+        src, lens = (torch.from_numpy(np.ascontiguousarray(a, np.int32)).to(tr.device) for a in (src_ids, src_len))
+        B, S = src.shape
+        out = torch.empty((B, max_len), dtype=torch.int32, device=tr.device)
+        length = torch.empty((B,), dtype=torch.int32, device=tr.device)
+        score = torch.empty((B,), dtype=torch.float32, device=tr.device)
+        torch.cuda.synchronize(tr.device)
+        tr._check(tr.lib.cmt_quant_beam_decode(tr.h, self.group, self.weights.data_ptr(), self.workspace.data_ptr(), src.data_ptr(), lens.data_ptr(),
+                                               B, S, max_len, beam, length_penalty, eos_id, out.data_ptr(), length.data_ptr(), score.data_ptr()))
+        return out.cpu().numpy(), length.cpu().numpy(), score.cpu().numpy()
+
+    def greedy_decode(self, src_ids, src_len, max_len, eos_id=3):
+        """As Trainer.greedy_decode: ids [B, max_len], lengths [B]."""
+        return self.beam_decode(src_ids, src_len, max_len, beam=1, length_penalty=0.0, eos_id=eos_id)[:2]
