@@ -210,7 +210,7 @@ size_t cache_attend_workspace(const CacheShape& s, int per, int q_heads, int tok
 
 struct AttendArgs {
   const void* q; size_t ldq; void* out; size_t ldo;
-  int per, share, splits, tokens, wide_q;
+  int per, share, splits, tokens, wide_q, wide_o;           // queries in aligned pieces of 8; results of 4
   float scale;
   float* ml; float* part;                                    // of splits: (maximum, sum) [unit][split][16], products [unit][split][16][64 chunks]
 };
@@ -226,11 +226,8 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
   __shared__ __align__(16) uint4 s_p[4 * PP * 64];
   __shared__ float s_f[16], s_l[16], s_m[16];
   const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int split = blockIdx.x % a.splits;
-  int u = blockIdx.x / a.splits;
-  const int unit = u, G = a.per * a.share, g_tiles = (G + 15) / 16;
-  const int g0 = (u % g_tiles) * 16; u /= g_tiles;
-  const int head = u % s.heads, b = u / s.heads;
+  const int split = blockIdx.x, G = a.per * a.share, g0 = blockIdx.y * 16, unit = blockIdx.z * gridDim.y + blockIdx.y;
+  const int b = s.heads == 1 ? blockIdx.z : blockIdx.z / s.heads, head = blockIdx.z - b * s.heads;
   const int len = min(c.lengths[b], a.tokens);
   const int chunks = s.chunks(), E = chunks * 2;
   const int span = ((len + ATTEND_CHUNK - 1) / ATTEND_CHUNK + a.splits - 1) / a.splits * ATTEND_CHUNK;   // of this sequence: equal shares
@@ -239,8 +236,9 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
   const char* const kc = c.k + at * chunks * 2048;
   const char* const vc = c.v + at * chunks * 2048;
   const int q4 = lane >> 4, g = lane & 15;
-  auto query = [&](int i) { return ((size_t)b * a.per + (g0 + i) / a.share); };   // row of query i of the tile
-  auto column = [&](int i) { return (size_t)(head * a.share + (g0 + i) % a.share) * s.dim; };
+  // row and column of the lane's query: number g of the tile
+  const int qr = a.share == 1 ? g0 + g : (g0 + g) / a.share;
+  const size_t row = (size_t)b * a.per + qr, column = (size_t)(head * a.share + (g0 + g - qr * a.share)) * s.dim;
   const int ts = E >= 6 ? 1 : 8 / E, mine = E >= 6 ? w * EPW : w % E, my_ts = E >= 6 ? 0 : w / E;   // columns 32 mine.., tokens' share
   v4f acc[EPW][2];
 #pragma unroll
@@ -263,15 +261,25 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
     ks = c.kscale[at + (tile >> 5)];
   };
   fetch_keys(first);
-  if (first < bound)
-    for (int i = t; i < chunks * 128; i += 64 * ATTEND_WAVES) {   // the queries as operands: [chunk][half][part][lane]
-      const int l = i & 63, ch = i >> 7, h = i >> 6 & 1, d = 64 * ch + 16 * (l >> 4) + 8 * h;
-      Frag<bf16_t> f[QP];
-      const bool in = g0 + (l & 15) < G && d < s.dim;
-      load_operand((const T*)a.q + (in ? query(l & 15) * a.ldq + column(l & 15) + d : 0), in ? s.dim - d : 0, a.wide_q, f);
+  if (first < bound) {                                       // the queries as operands: [chunk][half][part][lane]
+    Frag<T> raw[EPW];
+    const T* const qp = (const T*)a.q + (g0 + g < G ? row * a.ldq + column : 0);
 #pragma unroll
-      for (int p = 0; p < QP; ++p) s_q[((ch * 2 + h) * QP + p) * 64 + l] = f[p].v;
+    for (int u = 0; u < EPW; ++u) {                          // a thread's (lane, chunk, half) are those of its loads
+      const int i = u * 8 + w, d = 64 * (i >> 1) + 16 * q4 + 8 * (i & 1);
+      if (a.wide_q) raw[u].load(qp + (d < s.dim ? d : 0));
+      else load_elements(qp + d, g0 + g < G ? s.dim - d : 0, raw[u]);
     }
+#pragma unroll
+    for (int u = 0; u < EPW; ++u) {
+      const int i = u * 8 + w, d = 64 * (i >> 1) + 16 * q4 + 8 * (i & 1);
+      Frag<bf16_t> f[QP];
+      operand_of(raw[u], d < s.dim && g0 + g < G, f);
+      if (i < 2 * chunks)
+#pragma unroll
+        for (int p = 0; p < QP; ++p) s_q[(i * QP + p) * 64 + lane] = f[p].v;
+    }
+  }
   __syncthreads();
   for (int t0 = first; t0 < last; t0 += ATTEND_CHUNK) {
     const int tok = t0 + 4 * (t & 31);
@@ -405,16 +413,19 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
   }
   if (g0 + g >= G) return;
   const float sum = s_l[g], inv = sum == 0.f ? 0.f : 1.0f / sum;
-  T* const out = (T*)a.out + query(g) * a.ldo + column(g);
+  T* const out = (T*)a.out + row * a.ldo + column;
+  struct alignas(4 * sizeof(T)) Four { T v[4]; };
 #pragma unroll
   for (int e = 0; e < EPW; ++e)
     if (mine + e < E)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int d = 32 * (mine + e) + 16 * h + 4 * q4;
+        const Four o{{from_f<T>(acc[e][h][0] * inv), from_f<T>(acc[e][h][1] * inv), from_f<T>(acc[e][h][2] * inv), from_f<T>(acc[e][h][3] * inv)}};
+        if (a.wide_o) { if (d < s.dim) *reinterpret_cast<Four*>(out + d) = o; }
+        else
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (d + i < s.dim) out[d + i] = from_f<T>(acc[e][h][i] * inv);
+          for (int i = 0; i < 4; ++i) if (d + i < s.dim) out[d + i] = o.v[i];
       }
 }
 // joins the ranges of a query: one workgroup each, its threads a column of four and a share of the ranges
@@ -472,11 +483,12 @@ void launch_cache_attend(int prec, const CacheShape& s, const void* cache, const
   AttendArgs a{};
   a.q = q; a.ldq = ldq; a.out = out; a.ldo = ldo; a.per = per; a.share = q_heads / s.heads; a.splits = p.splits;
   a.tokens = tokens; a.scale = scale;
-  a.wide_q = (((uintptr_t)q | ldq * es | s.dim * es) & 15) == 0;
+  a.wide_q = (((uintptr_t)q | ldq * es) & 15) == 0 && s.dim % 8 == 0;
+  a.wide_o = (((uintptr_t)out | ldo * es | s.dim * es) & (4 * es - 1)) == 0;
   a.ml = (float*)workspace; a.part = a.ml + (size_t)units * p.splits * 32;
   auto go = [&](auto type, auto epw) {
     using T = decltype(type);
-    hipLaunchKernelGGL((cache_attend_kernel<T, decltype(epw)::value>), dim3((unsigned)(units * p.splits)), dim3(64 * ATTEND_WAVES), 0, st, a, s,
+    hipLaunchKernelGGL((cache_attend_kernel<T, decltype(epw)::value>), dim3(p.splits, p.g_tiles, s.seqs * s.heads), dim3(64 * ATTEND_WAVES), 0, st, a, s,
                        CacheView(s, const_cast<void*>(cache)));
     if (p.splits > 1) hipLaunchKernelGGL(cache_join_kernel<T>, dim3((unsigned)((long)s.seqs * s.heads * per * a.share)), dim3(256), 0, st, a, s);
   };

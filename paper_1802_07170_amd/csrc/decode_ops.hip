@@ -60,7 +60,10 @@ bool cache_shape(const cmt_cache_config* c, CacheShape* s) {
 bool attend_shape(const CacheShape& s, int32_t rows_per_sequence, int32_t query_heads, int32_t tokens) {
   if (rows_per_sequence < 1 || query_heads < 1 || query_heads % s.heads) { refuse("rows_per_sequence must be positive, query_heads a positive multiple of heads"); return false; }
   if (tokens < 1 || tokens > s.tokens) { refuse("tokens must be in [1, max_tokens]"); return false; }
-  if ((int64_t)s.seqs * rows_per_sequence * query_heads > 1 << 24) { refuse("more than 2^24 queries"); return false; }
+  if ((int64_t)s.seqs * rows_per_sequence * query_heads > 1 << 24 || (int64_t)rows_per_sequence * (query_heads / s.heads) > 1 << 19) {
+    refuse("more than 2^24 queries, or 2^19 of one sequence and head");
+    return false;
+  }
   return true;
 }
 

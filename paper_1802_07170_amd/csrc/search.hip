@@ -52,41 +52,40 @@ __global__ __launch_bounds__(256) void search_groups_kernel(const T* __restrict_
 }
 
 // ---- the choice --------------------------------------------------------------------------------------------
-constexpr int SELECT_NT = 1024, SELECT_NW = SELECT_NT / 64, SELECT_CAP = 1024;
+// One workgroup per sentence, a wavefront to a hypothesis (two where there are more than 16).  With 16 wavefronts every instruction takes 16 clocks of
+// the CU: what bounds this kernel is how many there are, so rows and groups go by wavefronts and lanes and by shifts, without divisions.
+constexpr int SELECT_WAVES = 16, SELECT_CAP = 1024, SELECT_BATCH = 8;
+constexpr int GROUP_BITS = 17, TOKEN_BITS = 26;              // (slot, group) and (slot, token) as ordered numbers
+static_assert(SEARCH_MAX_VOCAB == 1 << TOKEN_BITS && SEARCH_MAX_VOCAB / SEARCH_GROUP == 1 << GROUP_BITS && SEARCH_MAX == 32, "31 bits");
 __device__ __forceinline__ bool better(double a, unsigned ia, double b, unsigned ib) { return a > b || (a == b && ia < ib); }
 
 struct SelectShared {
   double base[SEARCH_MAX];
   double lv[SELECT_CAP]; unsigned li[SELECT_CAP];            // a list of candidates
   double wv[SEARCH_MAX]; unsigned wi[SEARCH_MAX];            // the best of them, in order
-  unsigned bound[SELECT_NW];
-  double rv[SELECT_NW]; unsigned ri[SELECT_NW];
+  unsigned bound[SELECT_WAVES];
+  double rv[SELECT_WAVES]; unsigned ri[SELECT_WAVES];
   int count;
 };
-// The n best of `total` items into sh.wv / sh.wi (returns how many there are).  value(i, index) gives an item's value (-inf: it does not
-// take part) and index.  least: items below it (as fp32) are known not to be among them.
-// Items that reach it are listed and each counts how many are better; a list that overflows - equal values in great number - is
-// answered by n rounds of a workgroup-wide maximum.
+// appends the candidates of the lanes with `take`: one atomic per wavefront
+__device__ __forceinline__ void select_append(SelectShared& sh, bool take, double v, unsigned index) {
+  const unsigned long long mask = __ballot(take);
+  if (!mask) return;
+  const int lane = threadIdx.x & 63;
+  int at = 0;
+  if (lane == 0) at = atomicAdd(&sh.count, __popcll(mask));
+  at = __builtin_amdgcn_readfirstlane(at) + __popcll(mask & ((1ull << lane) - 1));
+  if (take && at < SELECT_CAP) { sh.lv[at] = v; sh.li[at] = index; }
+}
+// The n best candidates into sh.wv / sh.wi (returns how many there are): each counts how many are better.  A list that has overflowed -
+// equal values in great number - is answered by n rounds of a maximum over all items: scan(f) passes a thread's items to f(value, index).
 template <typename F>
-__device__ __forceinline__ int select_best(SelectShared& sh, int n, int total, float least, F value) {
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  if (t == 0) sh.count = 0;
-  __syncthreads();
-  for (int i0 = 0; i0 < total; i0 += SELECT_NT) {
-    unsigned index = 0;
-    const double v = i0 + t < total ? value(i0 + t, index) : -INFINITY;
-    const bool take = v > -INFINITY && (float)v >= least;
-    const unsigned long long mask = __ballot(take);
-    if (!mask) continue;
-    int at = 0;
-    if (lane == 0) at = atomicAdd(&sh.count, __popcll(mask));
-    at = __builtin_amdgcn_readfirstlane(at) + __popcll(mask & ((1ull << lane) - 1));
-    if (take && at < SELECT_CAP) { sh.lv[at] = v; sh.li[at] = index; }
-  }
+__device__ __forceinline__ int select_best(SelectShared& sh, int n, F scan) {
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, threads = blockDim.x;
   __syncthreads();
   const int count = sh.count;
   if (count <= SELECT_CAP) {
-    for (int i = t; i < count; i += SELECT_NT) {
+    for (int i = t; i < count; i += threads) {
       const double v = sh.lv[i];
       const unsigned ix = sh.li[i];
       int place = 0;
@@ -99,15 +98,13 @@ __device__ __forceinline__ int select_best(SelectShared& sh, int n, int total, f
   }
   double last = INFINITY;
   unsigned last_index = 0;
+#pragma unroll 1
   for (int round = 0; round < n; ++round) {                  // (more than SELECT_CAP take part: there is a best one in each round)
     double bv = -INFINITY;
     unsigned bi = 0xffffffffu;
-#pragma unroll 1
-    for (int i = t; i < total; i += SELECT_NT) {
-      unsigned index = 0;
-      const double v = value(i, index);
+    scan([&](double v, unsigned index) {
       if (v > -INFINITY && (round == 0 || better(last, last_index, v, index)) && better(v, index, bv, bi)) { bv = v; bi = index; }
-    }
+    });
 #pragma unroll 1
     for (int o = 32; o > 0; o >>= 1) {
       const double ov = __shfl_xor(bv, o, 64);
@@ -118,7 +115,7 @@ __device__ __forceinline__ int select_best(SelectShared& sh, int n, int total, f
     __syncthreads();
     bv = sh.rv[0]; bi = sh.ri[0];
 #pragma unroll 1
-    for (int k = 1; k < SELECT_NW; ++k)
+    for (int k = 1; k < threads >> 6; ++k)
       if (better(sh.rv[k], sh.ri[k], bv, bi)) { bv = sh.rv[k]; bi = sh.ri[k]; }
     if (t == 0) { sh.wv[round] = bv; sh.wi[round] = bi; }
     last = bv; last_index = bi;
@@ -127,23 +124,28 @@ __device__ __forceinline__ int select_best(SelectShared& sh, int n, int total, f
   return n;
 }
 template <typename T, bool ADVANCE>
-__global__ __launch_bounds__(SELECT_NT) void search_select_kernel(const T* __restrict__ logits, size_t ld, const float* __restrict__ scores,
-                                                                  const float2* __restrict__ stat, int K, int V, int groups, int n,
-                                                                  float* __restrict__ out_scores, int32_t* __restrict__ out_rows,
-                                                                  int32_t* __restrict__ out_tokens, SearchAdvance adv) {
+__global__ __launch_bounds__(64 * SELECT_WAVES) void search_select_kernel(const T* __restrict__ logits, size_t ld, const float* __restrict__ scores,
+                                                                          const float2* __restrict__ stat, int K, int V, int groups, int n,
+                                                                          float* __restrict__ out_scores, int32_t* __restrict__ out_rows,
+                                                                          int32_t* __restrict__ out_tokens, SearchAdvance adv) {
   __shared__ SelectShared sh;
   __shared__ unsigned s_top[SEARCH_MAX];
-  const int b = blockIdx.x, t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), row0 = b * K;
-  for (int s = w; s < K; s += SELECT_NW) {                   // a row's score less its lse; -inf: it takes no part
+  const int b = blockIdx.x, t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), waves = blockDim.x >> 6, row0 = b * K;
+  if (t == 0) sh.count = 0;
+  // a row's score less its lse (-inf: it takes no part), and a bound: the n-th best of the lanes' best groups is one that n groups reach
+  unsigned bound = 0;
+  float x_first = -INFINITY;                                 // the lane's first group of the wavefront's first row
+  double base_first = -INFINITY;
+  for (int s = w; s < K; s += waves) {
     const float c = scores[row0 + s];
+    const float2* p = stat + (size_t)(row0 + s) * groups;
+    float2 x0 = p[min(lane, groups - 1)];                    // (asked for with the score; a dead row's: anything)
+    if (lane >= groups) x0 = make_float2(-INFINITY, 0.f);
     double base = -INFINITY;
+    float mine = x0.x;
     if (c > -INFINITY) {
-      const float2* p = stat + (size_t)(row0 + s) * groups;
-      const float2 x0 = lane < groups ? p[lane] : make_float2(-INFINITY, 0.f);
-      float mx = x0.x;
-      for (int g = lane + 64; g < groups; g += 64) mx = fmaxf(mx, p[g].x);
-      mx = lanes_max(mx);
-      const float ms = mx > -INFINITY ? mx : 0.f;
+      for (int g = lane + 64; g < groups; g += 64) mine = fmaxf(mine, p[g].x);
+      const float mx = lanes_max(mine), ms = mx > -INFINITY ? mx : 0.f;
       float sum = x0.x > -INFINITY ? x0.y * expf(x0.x - ms) : x0.y;
       for (int g = lane + 64; g < groups; g += 64) { const float2 x = p[g]; sum += x.x > -INFINITY ? x.y * expf(x.x - ms) : x.y; }
       sum = lanes_sum(sum);
@@ -151,46 +153,78 @@ __global__ __launch_bounds__(SELECT_NT) void search_select_kernel(const T* __res
       if (c < INFINITY && mx > -INFINITY && mx < INFINITY && sum < INFINITY) base = (double)c - (double)mx - (double)logf(sum);
     }
     if (lane == 0) sh.base[s] = base;
+    if (s == w) { x_first = x0.x; base_first = base; }
+    if (base > -INFINITY) {                                  // (uniform over the wavefront)
+      const unsigned key = mine > -INFINITY ? search_sortable((float)(base + (double)mine)) : 0u;
+      unsigned least = 0;
+#pragma unroll
+      for (int bit = 31; bit >= 0; --bit)
+        if (__popcll(__ballot(key >= (least | 1u << bit))) >= n) least |= 1u << bit;
+      bound = max(bound, least);
+    }
   }
+  if (lane == 0) sh.bound[w] = bound;
   __syncthreads();
-  const int total = K * groups;
-  auto group = [&](int i, unsigned& index) {
-    const int s = i / groups;
-    index = i;
-    const double base = sh.base[s];
-    return base > -INFINITY ? base + (double)stat[(size_t)row0 * groups + i].x : -(double)INFINITY;
-  };
-  // the n-th best of a wavefront's lanes' best is a bound that n groups reach
-  float tv = -INFINITY;
-  for (int i = t; i < total; i += SELECT_NT) { unsigned ix; tv = fmaxf(tv, (float)group(i, ix)); }
-  const unsigned key = search_sortable(tv);
-  unsigned least = 0;
-#pragma unroll
-  for (int bit = 31; bit >= 0; --bit)
-    if (__popcll(__ballot(key >= (least | 1u << bit))) >= n) least |= 1u << bit;
-  if (lane == 0) sh.bound[w] = least;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < SELECT_NW; ++i) least = max(least, sh.bound[i]);
-  const float bound = least < 0x00800000u ? -INFINITY : __uint_as_float((int)least < 0 ? least ^ 0x80000000u : ~least);
-  const int tops = select_best(sh, n, total, bound, group);
+  for (int i = 0; i < waves; ++i) bound = max(bound, sh.bound[i]);
+  const float reach = bound < 0x00800000u ? -INFINITY : __uint_as_float((int)bound < 0 ? bound ^ 0x80000000u : ~bound);
+  auto group_value = [&](double base, float x) { return base > -INFINITY ? base + (double)x : -(double)INFINITY; };
+  for (int s = w; s < K; s += waves) {
+    const double base = s == w ? base_first : sh.base[s];
+    if (!(base > -INFINITY)) continue;
+    for (int g = lane, g0 = 0; g0 < groups; g += 64, g0 += 64) {
+      const float x = g0 == 0 && s == w ? x_first : g < groups ? stat[(size_t)(row0 + s) * groups + g].x : -INFINITY;
+      const double v = group_value(base, x);
+      select_append(sh, v > -INFINITY && (float)v >= reach, v, (unsigned)s << GROUP_BITS | (unsigned)g);
+    }
+  }
+  const int tops = select_best(sh, n, [&](auto f) {
+#pragma unroll 1
+    for (int s = w; s < K; s += waves)
+#pragma unroll 1
+      for (int g = lane; g < groups; g += 64) f(group_value(sh.base[s], stat[(size_t)(row0 + s) * groups + g].x), (unsigned)s << GROUP_BITS | (unsigned)g);
+  });
+  const double least = tops == n ? sh.wv[n - 1] : -(double)INFINITY;
   if (t < tops) s_top[t] = sh.wi[t];
-  const float floor_ = tops == n ? (float)sh.wv[n - 1] : -INFINITY;
+  if (t == 0) sh.count = 0;
   __syncthreads();
-  const int found = tops == 0 ? 0 : select_best(sh, n, tops * SEARCH_GROUP, floor_, [&](int i, unsigned& index) {
-    const int id = s_top[i / SEARCH_GROUP], s = id / groups, v = (id - s * groups) * SEARCH_GROUP + i % SEARCH_GROUP;
-    index = (unsigned)s * (unsigned)V + (unsigned)v;
-    if (v >= V) return -(double)INFINITY;
-    const float z = to_f(logits[(size_t)(row0 + s) * ld + v]);
-    return z > -INFINITY ? sh.base[s] + (double)z : -(double)INFINITY;
+  // the entries of the best groups that reach the n-th group's best
+  const int entries = tops * SEARCH_GROUP, threads = blockDim.x;
+  auto entry = [&](int i, unsigned& index) {                 // its logit (-inf: there is none)
+    const unsigned id = s_top[i / SEARCH_GROUP], s = id >> GROUP_BITS, v = (id & ((1u << GROUP_BITS) - 1)) * SEARCH_GROUP + i % SEARCH_GROUP;
+    index = s << TOKEN_BITS | v;
+    return v < (unsigned)V ? to_f(logits[(size_t)(row0 + s) * ld + v]) : -INFINITY;
+  };
+  for (int i0 = 0; i0 < entries; i0 += SELECT_BATCH * threads) {
+    float z[SELECT_BATCH];
+    unsigned index[SELECT_BATCH];
+#pragma unroll
+    for (int u = 0; u < SELECT_BATCH; ++u) {                 // (all on their way before the first is looked at)
+      z[u] = -INFINITY; index[u] = 0;
+      const int i = i0 + u * threads + t;
+      if (i0 + u * threads < entries && i < entries) z[u] = entry(i, index[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < SELECT_BATCH; ++u) {
+      if (i0 + u * threads >= entries) break;
+      const double v = sh.base[index[u] >> TOKEN_BITS] + (double)z[u];
+      select_append(sh, z[u] > -INFINITY && v >= least, v, index[u]);   // (a logit of NaN makes its row's lse one: not here)
+    }
+  }
+  const int found = select_best(sh, n, [&](auto f) {
+#pragma unroll 1
+    for (int i = t; i < entries; i += threads) {
+      unsigned index;
+      const float z = entry(i, index);
+      f(z > -INFINITY ? sh.base[index >> TOKEN_BITS] + (double)z : -(double)INFINITY, index);
+    }
   });
   if (!ADVANCE) {
     if (t < n) {
       const bool in = t < found;
-      const unsigned ix = in ? sh.wi[t] : 0, s = ix / (unsigned)V;
+      const unsigned ix = in ? sh.wi[t] : 0, s = ix >> TOKEN_BITS;
       out_scores[(size_t)b * n + t] = in ? (float)sh.wv[t] : -INFINITY;
       out_rows[(size_t)b * n + t] = in ? row0 + (int)s : -1;
-      out_tokens[(size_t)b * n + t] = in ? (int)(ix - s * (unsigned)V) : -1;
+      out_tokens[(size_t)b * n + t] = in ? (int)(ix & ((1u << TOKEN_BITS) - 1)) : -1;
     }
     return;
   }
@@ -199,7 +233,7 @@ __global__ __launch_bounds__(SELECT_NT) void search_select_kernel(const T* __res
   const bool won = t < found;
   const double v = won ? sh.wv[t] : -INFINITY;
   const unsigned ix = won ? sh.wi[t] : 0;
-  const int s = ix / (unsigned)V, tk = ix - (unsigned)s * (unsigned)V;
+  const int s = ix >> TOKEN_BITS, tk = ix & ((1u << TOKEN_BITS) - 1);
   const bool fin = won && (tk == adv.eos || adv.j == adv.max_len - 1), live = won && !fin;
   const unsigned long long m_fin = __ballot(fin), m_live = __ballot(live);
   const int n_new = __popcll(m_live);
@@ -231,15 +265,15 @@ void launch_search_select(int prec, const void* logits, size_t ld, const float* 
   const int groups = search_groups(V);
   const int wide = (((uintptr_t)logits | ld * (prec ? 2 : 4)) & 15) == 0;
   float2* stat = (float2*)workspace;
-  const dim3 grid((unsigned)(((long)B * K * groups + 3) / 4));
+  const dim3 grid((unsigned)(((long)B * K * groups + 3) / 4)), threads(64 * std::min(SELECT_WAVES, std::max(4, K)));
   auto go = [&](auto type) {
     using T = decltype(type);
     hipLaunchKernelGGL(search_groups_kernel<T>, grid, dim3(256), 0, st, (const T*)logits, ld, scores, B * K, V, groups, wide, stat);
     if (adv)
-      hipLaunchKernelGGL((search_select_kernel<T, true>), dim3(B), dim3(SELECT_NT), 0, st, (const T*)logits, ld, scores, stat, K, V, groups, n, out_scores,
+      hipLaunchKernelGGL((search_select_kernel<T, true>), dim3(B), threads, 0, st, (const T*)logits, ld, scores, stat, K, V, groups, n, out_scores,
                          out_rows, out_tokens, *adv);
     else
-      hipLaunchKernelGGL((search_select_kernel<T, false>), dim3(B), dim3(SELECT_NT), 0, st, (const T*)logits, ld, scores, stat, K, V, groups, n, out_scores,
+      hipLaunchKernelGGL((search_select_kernel<T, false>), dim3(B), threads, 0, st, (const T*)logits, ld, scores, stat, K, V, groups, n, out_scores,
                          out_rows, out_tokens, SearchAdvance{});
   };
   if (prec) go(bf16_t{}); else go(float{});
