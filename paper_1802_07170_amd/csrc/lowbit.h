@@ -35,7 +35,7 @@ void launch_quant_cell(int prec, const float* gates, const float* c_prev, float*
 
 // ---- cache.hip: source rows in 8 bits -------------------------------------------------------------
 // Per (sequence, head, block of 32 tokens) one fp32 scale for the keys and one for the values; codes are whole numbers -127..127.
-// Keys: tiles of 16 tokens x 64 d, 1 KB, lane l's 16 bytes being token l % 16, d = 16 (l / 16) + 0..15.
+// Keys: tiles of 32 tokens x 32 d, 1 KB, lane l's bytes 8 h + j (h = 0, 1) being token 16 h + l % 16, d = 8 (l / 16) + j: two operands of 16 tokens.
 // Values: tiles of 32 tokens x 32 d, 1 KB, lane l's bytes 8 h + j (h = 0, 1) being d = 16 h + l % 16 and token 4 (l / 16) + j (j < 4)
 // or 12 + 4 (l / 16) + j: the order in which the scores' accumulators hold the tokens, so that weights go from one
 // product into the other without leaving their lanes.
@@ -43,11 +43,11 @@ constexpr int CACHE_BLOCK = 32;
 struct CacheShape {
   int seqs, heads, dim, tokens;                            // tokens: the capacity
   __host__ __device__ int blocks() const { return (tokens + CACHE_BLOCK - 1) / CACHE_BLOCK; }
-  __host__ __device__ int chunks() const { return (dim + 63) / 64; }           // of 64 d
+  __host__ __device__ int chunks() const { return (dim + 31) / 32; }           // of 32 d
   size_t part() const { return (size_t)seqs * heads * blocks(); }
   size_t lengths_bytes() const { return ((size_t)seqs * 4 + 255) & ~(size_t)255; }
   size_t scales_bytes() const { return (part() * 4 + 255) & ~(size_t)255; }
-  size_t codes_bytes() const { return part() * chunks() * 2048; }
+  size_t codes_bytes() const { return part() * chunks() * 1024; }
   size_t bytes() const { return lengths_bytes() + 2 * scales_bytes() + 2 * codes_bytes(); }
 };
 struct CacheView {

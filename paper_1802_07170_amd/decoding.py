@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import struct
 
 import numpy as np
 import torch
@@ -250,38 +251,38 @@ def beam_reorder(rows, sources, targets):
     tensors' first dimension counting rows, the others contiguous.  Target rows whose number is outside the source stay as they were."""
     if not isinstance(rows, torch.Tensor) or rows.dtype != torch.int32 or not rows.is_contiguous() or not rows.is_cuda:
         raise ValueError("rows must be a contiguous int32 tensor on a GPU")
-    if len(sources) != len(targets) or not all(isinstance(t, torch.Tensor) and t.dim() for t in (*sources, *targets)):
-        raise ValueError("sources and targets must be as many tensors, of one dimension at least")
+    if len(sources) != len(targets):
+        raise ValueError(f"{len(sources)} sources and {len(targets)} targets")
     if not sources:
         return
-    count, source_rows, device, grad = rows.numel(), len(sources[0]), rows.device, torch.is_grad_enabled()
+    count, source_rows, device, grad = rows.numel(), sources[0].shape[:1], rows.device, torch.is_grad_enabled()
+    source_rows = source_rows[0] if source_rows else -1
     fields = []                                            # of a CmtReorderTensor each: five numbers of 64 bits
     for i, (a, b) in enumerate(zip(sources, targets)):
         sa, sb = a.shape, b.shape
-        if sa[0] != source_rows or sb[0] != count or (sa != sb if count == source_rows else sa[1:] != sb[1:]):
+        if not sa or not sb or sa[0] != source_rows or sb[0] != count or (sa != sb if count == source_rows else sa[1:] != sb[1:]):
             raise ValueError(f"tensors {i} must have {source_rows} and {count} rows alike, not {tuple(sa)} and {tuple(sb)}")
         if a.dtype != b.dtype or a.device != device or b.device != device:
             raise ValueError(f"tensors {i} must be of one type and on the device of rows")
         if grad and (a.requires_grad or b.requires_grad):
             raise ValueError(f"tensors {i} want a gradient: these operators have none (use torch.no_grad())")
-        size = a.element_size()
-        width = a.numel() // source_rows * size if source_rows else 0
+        width = a.nbytes // source_rows if source_rows else 0
         if width:
-            fields += (a.data_ptr(), b.data_ptr(), width if a.is_contiguous() else _row_pitch(a, i) * size,
-                       width if b.is_contiguous() else _row_pitch(b, i) * size, width)
+            fields += (a.data_ptr(), b.data_ptr(), width if a.is_contiguous() else _row_pitch(a, i),
+                       width if b.is_contiguous() else _row_pitch(b, i), width)
     if not fields or not count:
         return
-    _call(binding.load_library().cmt_beam_reorder, device, rows.data_ptr(), count, source_rows, (C.c_int64 * len(fields))(*fields), len(fields) // 5)
+    _call(binding.load_library().cmt_beam_reorder, device, rows.data_ptr(), count, source_rows, struct.pack(f"{len(fields)}q", *fields), len(fields) // 5)
 
 
 def _row_pitch(t, i):
-    """Elements from one row (first dimension) to the next, whose own elements lie side by side."""
+    """Bytes from one row (first dimension) to the next, whose own elements lie side by side."""
     side = 1
     for d in range(t.dim() - 1, 0, -1):
         if t.shape[d] > 1 and t.stride(d) != side:
             raise ValueError(f"tensors {i}: the elements of a row must lie side by side")
         side *= t.shape[d]
-    return t.stride(0) if t.shape[0] > 1 else side
+    return (t.stride(0) if t.shape[0] > 1 else side) * t.element_size()
 
 
 class QuantDecoder:

@@ -154,7 +154,8 @@ def plain_cache(x, lengths):
     return out
 
 
-@pytest.mark.parametrize("b,s,h,d", [(1, 1, 1, 1), (3, 33, 1, 16), (4, 64, 2, 40), (2, 70, 3, 64), (5, 31, 1, 336), (2, 100, 1, 1024)])
+@pytest.mark.parametrize("b,s,h,d", [(1, 1, 1, 1), (3, 33, 1, 16), (4, 64, 2, 40), (2, 70, 3, 64), (5, 31, 1, 336), (2, 100, 1, 1024),
+                                     (3, 300, 2, 8), (2, 200, 1, 96), (4, 129, 2, 120), (2, 65, 2, 33), (2, 40, 1, 520)])
 @pytest.mark.parametrize("dtype", [BF, FP])
 def test_cache_holds_the_nearest_codes(D, b, s, h, d, dtype):
     k, v = randn(b + s, b, s, h, d).to(dtype), (3 * randn(b + s + 1, b, s, h, d)).to(dtype)
@@ -211,7 +212,8 @@ def attend_plain(q, k, v, lengths, scale):
 
 @pytest.mark.parametrize("b,per,kv,share,d,lengths", [
     (1, 1, 1, 1, 16, [1]), (2, 3, 1, 1, 64, [0, 31]), (3, 10, 1, 1, 1024, [50, 1, 33]), (2, 16, 1, 1, 336, [32, 37]), (2, 17, 1, 1, 100, [129, 127]),
-    (1, 1, 4, 4, 128, [700]), (2, 5, 2, 3, 64, [130, 400]), (1, 2, 1, 1, 512, [1500]), (3, 1, 2, 8, 192, [0, 128, 300]), (1, 40, 1, 1, 256, [260]), (1, 2, 3, 1, 1, [40])])
+    (1, 1, 4, 4, 128, [700]), (2, 5, 2, 3, 64, [130, 400]), (1, 2, 1, 1, 512, [1500]), (3, 1, 2, 8, 192, [0, 128, 300]), (1, 40, 1, 1, 256, [260]), (1, 2, 3, 1, 1, [40]),
+    (2, 20, 2, 2, 32, [257, 600]), (1, 3, 1, 8, 80, [513]), (2, 33, 1, 1, 96, [65, 256]), (3, 18, 1, 1, 500, [129, 0, 40]), (1, 5, 2, 1, 48, [70]), (1, 17, 1, 2, 768, [200])])
 @pytest.mark.parametrize("dtype", [BF, FP])
 def test_attention(D, b, per, kv, share, d, lengths, dtype):
     s = max(lengths)
