@@ -283,7 +283,8 @@ int cmt_quant_weight_encode(const uint8_t* codes_dev, const uint16_t* scales_dev
                             void* hip_stream);
 int cmt_quant_weight_values(const void* packed_dev, int32_t outputs, int32_t inputs, int32_t group, float* weight_dev, void* hip_stream);
 /* y[m, n] = f(sum_k x[m, k] W[n, k] + bias[n]), f = tanh where tanh_of is not 0; bias_dev (fp32) may be NULL.  x of `type`, y of y_type (CMT_FP32
- * or CMT_BF16), row-major with pitches in elements; 0 <= rows <= 65535 (0: nothing is done).  Products are exact, sums fp32 in either type. */
+ * or CMT_BF16), row-major with pitches in elements; 0 <= rows <= 65535 (0: nothing is done); y shares no memory with x.  Products are exact, sums fp32 in either
+ * type, in an order that the sizes alone decide. */
 int cmt_quant_product(const void* x_dev, int32_t type, int64_t x_pitch, int32_t rows, const void* packed_dev, int32_t outputs, int32_t inputs,
                       int32_t group, const float* bias_dev, int32_t tanh_of, void* y_dev, int32_t y_type, int64_t y_pitch, void* hip_stream);
 
@@ -317,7 +318,7 @@ int cmt_beam_select_workspace(int32_t sentences, int32_t beam, int32_t vocab, si
 int cmt_beam_select(const void* logits_dev, int32_t type, int64_t pitch, const float* scores_dev, int32_t sentences, int32_t beam, int32_t vocab,
                     int32_t n, float* out_scores_dev, int32_t* out_rows_dev, int32_t* out_tokens_dev, void* workspace_dev, size_t workspace_bytes,
                     void* hip_stream);
-/* target[r] = source[rows[r]] for r < count, of n tensors of rows of row_bytes (pitches in bytes; `tensors` is host memory, read before the call
+/* target[r] = source[rows[r]] for r < count, of n <= 256 tensors of rows of row_bytes (pitches in bytes; `tensors` is host memory, read before the call
  * returns).  A row whose number is outside [0, source_rows) is left as it was.  No target may overlap a source or another target. */
 typedef struct cmt_reorder_tensor { const void* source_dev; void* target_dev; int64_t source_pitch, target_pitch, row_bytes; } cmt_reorder_tensor;
 int cmt_beam_reorder(const int32_t* rows_dev, int32_t count, int32_t source_rows, const cmt_reorder_tensor* tensors, int32_t n, void* hip_stream);

@@ -12,12 +12,36 @@
 
 namespace cmt {
 
-// Nearest whole number to x / s, the even one of two, as if the quotient were exact.  inv ~ 1 / s.
-__device__ __forceinline__ float cache_code(float x, float s, float inv) {
-  float q = rintf(x * inv);
+// Nearest whole number to x / s, the even one of two, as if the quotient were exact.
+__device__ __forceinline__ int cache_code(float x, float s) {
+  if (s < 1e-36f) return (int)fmin(fmax(rint((double)x / (double)s), -127.0), 127.0);   // (1 / s may be infinite, s a rounded subnormal number)
+  float q = rintf(x / s);
   const float r = fmaf(-q, s, x), r2 = 2.f * fabsf(r);       // (exact: |r| < 2 s and a multiple of half an ulp of s)
   if (r2 > s || (r2 == s && ((int)q & 1))) q += copysignf(1.f, r);
-  return fminf(fmaxf(q, -127.f), 127.f);
+  return (int)q;
+}
+// The same of 16 numbers, packed: x inv + 1.5 2^23 has the code in its lowest bits, and is right wherever the remainder stays below half
+// a step; a slot with one that does not (a tie, or inv's rounding next to one) is made number by number.  (That for all: three times the instructions, which
+// bound the fill: 128 x 55 x 1024 31 us.)
+template <typename T>
+__device__ __forceinline__ void cache_codes(const Frag<T> (&x)[2], float s, float inv, uint32_t (&o)[4]) {
+  const float big = 12582912.f;
+  float worst = 0.f;
+  uint32_t c[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const float v = x[e >> 3].get(e & 7), y = fmaf(v, inv, big);
+    worst = fmaxf(worst, fabsf(fmaf(-(y - big), s, v)));
+    c[e] = __float_as_uint(y);
+  }
+  if (s < 1e-36f || !(2.f * worst < s))
+#pragma unroll
+    for (int e = 0; e < 16; ++e) c[e] = (uint32_t)cache_code(x[e >> 3].get(e & 7), s);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t lo = __builtin_amdgcn_perm(c[4 * k + 1], c[4 * k], 0x0c0c0400), hi = __builtin_amdgcn_perm(c[4 * k + 3], c[4 * k + 2], 0x04000c0c);
+    o[k] = lo | hi;
+  }
 }
 
 // ---- writing ---------------------------------------------------------------------------------------------
@@ -33,8 +57,7 @@ __host__ __device__ inline int fill_blocks(int chunks) { return chunks > 4 ? 1 :
 template <typename T, int NS>
 __global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const int32_t* __restrict__ lengths, int tokens, CacheShape s, CacheView c, int wide) {
   __shared__ uint4 code[512 * NS];                           // in the cache's order
-  __shared__ float s_most[8];
-  __shared__ int s_bad[8];
+  __shared__ uint32_t s_most[8];
   const int b = s.heads == 1 ? blockIdx.y : blockIdx.y / s.heads, head = blockIdx.y - b * s.heads, t = threadIdx.x, lane = t & 63;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const bool is_v = blockIdx.z;
@@ -50,8 +73,7 @@ __global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const 
                (size_t)blk * CACHE_BLOCK * tok;
   const bool wd = wide >> is_v & 1;
   Frag<T> x[NS][2];                                          // as they come: 16-bit ones take half the registers
-  float most = 0.f;
-  bool bad = false;
+  uint32_t bits = 0;                                         // the largest without its sign: as numbers, infinities and NaN above all
 #pragma unroll
   for (int k = 0; k < NS; ++k) {
     const int i = k * 512 + i0, r = i & 31, d = 16 * (i >> 5);
@@ -60,21 +82,18 @@ __global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const 
 #pragma unroll
   for (int k = 0; k < NS; ++k)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float a = fabsf(x[k][e >> 3].get(e & 7));
-      most = fmaxf(most, a);
-      bad |= !(a <= 3.4028235e38f);
-    }
-  most = lanes_max(most);
-  const bool any = __ballot(bad) != 0;
-  if (lane == 0) { s_most[w] = most; s_bad[w] = any; }
+    for (int e = 0; e < 16; ++e) bits = max(bits, __float_as_uint(x[k][e >> 3].get(e & 7)) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) bits = max(bits, (uint32_t)__shfl_xor((int)bits, o, 64));
+  if (lane == 0) s_most[w] = bits;
   __syncthreads();
-  bool finite = true;
-  for (int k = w0; k < min(w0 + wn, 8); ++k) { most = fmaxf(most, s_most[k]); finite &= !s_bad[k]; }
+  for (int k = w0; k < min(w0 + wn, 8); ++k) bits = max(bits, s_most[k]);
+  const bool finite = bits < 0x7f800000u;
+  const float most = __uint_as_float(bits);
   const float scale = finite ? most / 127.0f : __uint_as_float(0x7fc00000u);   // (a block with a number that is none: no result hides it)
   const size_t at = ((size_t)b * s.heads + head) * s.blocks() + blk;
   if (i0 == 0 && n > 0) (is_v ? c.vscale : c.kscale)[at] = scale;
-  const bool some = scale > 0.f, tiny = scale < 1e-36f;
+  const bool some = scale > 0.f;
   const float inv = 1.0f / scale;
   char* const out = (is_v ? c.v : c.k) + at * chunks * 1024;
   uint4* const block = code + 64 * w0;
@@ -82,20 +101,7 @@ __global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const 
   for (int k = 0; k < NS; ++k) {
     const int i = k * 512 + i0, r = i & 31, d16 = i >> 5;
     uint32_t o[4] = {0, 0, 0, 0};
-    if (tiny && some) {                                      // (uniform; 1 / scale may be infinite)
-#pragma unroll 1
-      for (int e = 0; e < 16; ++e) {
-        float y = 0.f;
-#pragma unroll
-        for (int f = 0; f < 16; ++f) y = f == e ? x[k][f >> 3].get(f & 7) : y;
-        const uint32_t q = (uint32_t)((int)fmin(fmax(rint((double)y / (double)scale), -127.0), 127.0) & 255) << (8 * (e & 3));
-#pragma unroll
-        for (int f = 0; f < 4; ++f) o[f] |= f == e >> 2 ? q : 0u;
-      }
-    } else if (some) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[e >> 2] |= (uint32_t)((int)cache_code(x[k][e >> 3].get(e & 7), scale, inv) & 255) << (8 * (e & 3));
-    }
+    if (some) cache_codes(x[k], scale, inv, o);
     if (!is_v) {
       if (i < slots) {                                       // two lanes' pieces of 8 d
         uint2* const to = reinterpret_cast<uint2*>(block) + ((d16 >> 1) * 64 + 32 * (d16 & 1) + (r & 15)) * 2 + (r >> 4);

@@ -212,7 +212,7 @@ int cmt_beam_select(const void* logits_dev, int32_t type, int64_t pitch, const f
   return done("cmt_beam_select");
 }
 int cmt_beam_reorder(const int32_t* rows_dev, int32_t count, int32_t source_rows, const cmt_reorder_tensor* tensors, int32_t n, void* hip_stream) {
-  if (n < 0 || count < 0 || source_rows < 0) return refuse("counts must not be negative");
+  if (n < 0 || n > 256 || count < 0 || source_rows < 0) return refuse("counts must not be negative, tensors at most 256");
   if (n == 0 || count == 0) return CMT_OK;
   if (!rows_dev || !tensors) return refuse("null pointer");
   if (misaligned(rows_dev, 4)) return refuse("rows are 4-byte aligned");

@@ -230,7 +230,9 @@ __global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T*
                                                                  size_t ldy) {
   constexpr int PARTS = OPERAND_PARTS<T>, PER = QUANT_TILE_K / GROUP, STEPS = GROUP / 32, WN = 4, NT = 4;
   constexpr bool DIRECT = WHOLE && sizeof(T) == 2;
-  constexpr int THREADS = QUANT_WIDE, SLOTS = 2 * MT * 4 * 64, MINE = SLOTS / THREADS;   // 16 bytes (a part) of x each: [tile of rows][step][lane]
+  constexpr int THREADS = QUANT_WIDE, SLOTS = 2 * MT * 4 * 64, MINE = SLOTS / THREADS;
+  // Slots of 8 k of x: row slot / 16, and in it chunk (slot ^ row) % 16 - a load takes whole lines of four rows, and the 16 rows of an operand lie
+  // in 16 different banks' worth of LDS.  (16 rows x 64 bytes to a load, in operand order: 5 of 67 us more.)
   __shared__ uint4 xs[2][PARTS][SLOTS];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wn = w >> 1, wm = w & 1;
   const int id = blockIdx.x, seq = id >> 3, mb = seq % m_blocks, nb = ((seq / m_blocks) * 8 + (id & 7)) * NT * WN + wn * NT;
@@ -250,13 +252,14 @@ __global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T*
   const bf16_t* const sp = scales + 4 * q;
   // 16-bit rows of whole pieces go from memory to LDS without passing registers (the instruction is written out because the compiler would
   // wait for it before the next read of LDS); the last tile's pieces behind K are zeros.
+  auto chunk_of = [](int slot) { return (slot ^ slot >> 4) & 15; };
   unsigned off[MINE];
   const char* const xb = (const char*)(x + (size_t)m0 * ldx);
   if constexpr (DIRECT) {
 #pragma unroll
     for (int u = 0; u < MINE; ++u) {
-      const int slot = u * THREADS + threadIdx.x, l = slot & 63, m = min(m0 + 16 * (slot >> 8) + (l & 15), M - 1) - m0;
-      off[u] = ((unsigned)m * (unsigned)ldx + 32 * (slot >> 6 & 3) + 8 * (l >> 4)) * 2;
+      const int slot = u * THREADS + threadIdx.x, m = min(m0 + (slot >> 4), M - 1) - m0;
+      off[u] = ((unsigned)m * (unsigned)ldx + 8 * chunk_of(slot)) * 2;
     }
   }
   auto request = [&](int kt, uint4* to) {
@@ -271,7 +274,7 @@ __global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T*
 #pragma unroll
       for (int u = 0; u < MINE; ++u) {
         const int slot = u * THREADS + threadIdx.x;
-        const bool in = kt * QUANT_TILE_K + 32 * (slot >> 6 & 3) + 8 * (slot >> 4 & 3) < K;
+        const bool in = kt * QUANT_TILE_K + 8 * chunk_of(slot) < K;
         to[slot] = in ? *reinterpret_cast<const uint4*>(src + off[u]) : make_uint4(0, 0, 0, 0);
       }
     }
@@ -287,8 +290,7 @@ __global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T*
     if constexpr (DIRECT) return;
 #pragma unroll
     for (int u = 0; u < MINE; ++u) {
-      const int slot = u * THREADS + threadIdx.x, l = slot & 63, s = slot >> 6 & 3, m = m0 + 16 * (slot >> 8) + (l & 15);
-      const int k = kt * QUANT_TILE_K + 32 * s + 8 * (l >> 4);
+      const int slot = u * THREADS + threadIdx.x, m = m0 + (slot >> 4), k = kt * QUANT_TILE_K + 8 * chunk_of(slot);
       if constexpr (WHOLE) xn[u].load(x + (size_t)min(m, M - 1) * ldx + (k < K ? k : 0));   // (rows beyond M: not stored)
       else load_elements(x + (m < M ? (size_t)m * ldx + k : 0), m < M ? K - k : 0, xn[u]);
     }
@@ -302,7 +304,7 @@ __global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T*
     for (int u = 0; u < MINE; ++u) {
       const int slot = u * THREADS + threadIdx.x;
       Frag<bf16_t> f[PARTS];
-      operand_of(xn[u], !WHOLE || kt * QUANT_TILE_K + 32 * (slot >> 6 & 3) + 8 * (slot >> 4 & 3) < K, f);
+      operand_of(xn[u], !WHOLE || kt * QUANT_TILE_K + 8 * chunk_of(slot) < K, f);
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) buf[p][slot] = f[p].v;
     }
@@ -328,31 +330,37 @@ __global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T*
     Frag<bf16_t> xf[2][PARTS];
     auto read = [&](int i, Frag<bf16_t> (&f)[PARTS]) {
 #pragma unroll
-      for (int p = 0; p < PARTS; ++p) f[p].v = buf[p][(wm * SEQ + i) * 64 + lane];
+      for (int p = 0; p < PARTS; ++p) f[p].v = buf[p][(wm * MT + (i >> 2)) * 256 + c * 16 + ((4 * (i & 3) + q) ^ c)];
     };
     read(0, xf[0]);
-    v4f part[NT];
+    // a group's sums are scaled while the next group's products are being made
+    v4f part[2][NT];
+    auto scale = [&](int group) {
+      const int j = group / PER, g = group % PER;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const v4f& y = part[group & 1][n];
+        acc[n][j][0] = fmaf(y[0], __uint_as_float(sc[n][g].x << 16), acc[n][j][0]);
+        acc[n][j][1] = fmaf(y[1], __uint_as_float(sc[n][g].x & 0xffff0000u), acc[n][j][1]);
+        acc[n][j][2] = fmaf(y[2], __uint_as_float(sc[n][g].y << 16), acc[n][j][2]);
+        acc[n][j][3] = fmaf(y[3], __uint_as_float(sc[n][g].y & 0xffff0000u), acc[n][j][3]);
+      }
+    };
 #pragma unroll
     for (int i = 0; i < SEQ; ++i) {
-      const int j = i >> 2, s = i & 3, g = s / STEPS;
+      const int s = i & 3, group = i / STEPS;
       if (i + 1 < SEQ) read(i + 1, xf[(i + 1) & 1]);
       __builtin_amdgcn_sched_barrier(0);
-      if (s % STEPS == 0)
+      if (i % STEPS == 0)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) part[n] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < NT; ++n) part[group & 1][n] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int p = PARTS - 1; p >= 0; --p)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) mma16(part[n], wf[n][s], xf[i & 1][p]);
-      if (s % STEPS == STEPS - 1)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          acc[n][j][0] = fmaf(part[n][0], __uint_as_float(sc[n][g].x << 16), acc[n][j][0]);
-          acc[n][j][1] = fmaf(part[n][1], __uint_as_float(sc[n][g].x & 0xffff0000u), acc[n][j][1]);
-          acc[n][j][2] = fmaf(part[n][2], __uint_as_float(sc[n][g].y << 16), acc[n][j][2]);
-          acc[n][j][3] = fmaf(part[n][3], __uint_as_float(sc[n][g].y & 0xffff0000u), acc[n][j][3]);
-        }
+        for (int n = 0; n < NT; ++n) mma16(part[group & 1][n], wf[n][s], xf[i & 1][p]);
+      if (i % STEPS == 0 && group > 0) scale(group - 1);
     }
+    scale(SEQ / STEPS - 1);
   }
 #pragma unroll
   for (int i = 0; i < NT; ++i) {

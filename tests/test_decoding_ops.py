@@ -91,7 +91,8 @@ def product_bound(x, w, bias, want, dtype, out_dtype):
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 16, 128), (2, 15, 7), (3, 17, 31), (16, 40, 33), (17, 100, 129), (1, 4096, 300), (5, 8200, 260), (33, 8200, 130),
-                                   (70, 100, 1100), (130, 48, 64), (40, 8208, 2050)])
+                                   (70, 100, 1100), (130, 48, 64), (40, 8208, 2050),
+                                   (390, 8208, 133), (640, 8208, 130), (450, 8200, 264), (1000, 4100, 72)])     # (these fill the chip with 64 rows to a workgroup, or more)
 @pytest.mark.parametrize("dtype,out_dtype,group,bias,tanh", [(BF, FP, 64, True, False), (BF, BF, 32, False, True), (FP, FP, 128, True, False), (FP, FP, 32, False, True),
                                                              (FP, BF, 64, True, False)])
 def test_product(D, m, n, k, dtype, out_dtype, group, bias, tanh):
@@ -119,6 +120,22 @@ def test_product_of_strided_rows_leaves_its_neighbours_alone(D, dtype):
     out[1:21, 3:53] = 7.0
     assert (out == 7.0).all()
     assert D.quant_product(dev(big)[:0, 7:207], weight).shape == (0, 50)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_product_does_not_see_what_is_beside_its_rows(D, dtype):
+    for m, n, k in ((5, 100, 72), (20, 9000, 40), (390, 8208, 136), (650, 8208, 200), (390, 8208, 131)):
+        wide = torch.full((m + 3, k + 24), math.nan, dtype=dtype, device="cuda")
+        weight = D.QuantWeight.pack(dev(0.1 * randn(n, n, k)), 128)
+        for at in (8, 3):                                    # rows that begin at whole 16 bytes, and elsewhere
+            wide.fill_(math.nan)
+            x = wide[1:m + 1, at:at + k]
+            x.copy_(dev(randn(m, m, k), dtype))
+            out = torch.full((m + 2, n + 8), 7.0, device="cuda")
+            D.quant_product(x, weight, out=out[1:-1, 4:-4])
+            assert torch.equal(out[1:-1, 4:-4], D.quant_product(x.contiguous(), weight, out_dtype=FP))
+            out[1:-1, 4:-4] = 7.0
+            assert (out == 7.0).all()
 
 
 @pytest.mark.parametrize("dtype", [BF, FP])

@@ -85,6 +85,7 @@ def test_the_search_s_arguments(lib):
         assert lib.cmt_beam_reorder(AT, 4, 4, job, 1, None) == E
     fine = one(AT, 2 * AT, 8, 8, 8)
     assert lib.cmt_beam_reorder(None, 4, 4, fine, 1, None) == E and lib.cmt_beam_reorder(AT, -1, 4, fine, 1, None) == E
+    assert lib.cmt_beam_reorder(AT, 4, 4, fine, 257, None) == E and "256" in text(lib)
     assert lib.cmt_beam_reorder(AT, 0, 4, fine, 1, None) == 0 and lib.cmt_beam_reorder(AT, 4, 4, None, 0, None) == 0
 
 
