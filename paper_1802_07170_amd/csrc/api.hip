@@ -1858,10 +1858,10 @@ struct QuantDecoder {
 };
 // What one search keeps beside the handle's workspace, for R rows: the operands [embedding; H_o; h] and [input; h] of the layers and
 // [C_s; H_t] of the attentional layer, states and H_o that a position makes (the choice of hypotheses moves them to where the next one
-// reads them), gates, logits, the source rows in 8 bits.
+// reads them), logits, the source rows in 8 bits.
 struct QuantSearch {
   char* xcat = nullptr; char* xl[8] = {}; char* xc = nullptr; char* hn[8] = {}; char* ho = nullptr;
-  float* c[8] = {}; float* cn[8] = {}; float* gates = nullptr; float* logits = nullptr;
+  float* c[8] = {}; float* cn[8] = {}; float* logits = nullptr;
   void* cache = nullptr; void* attend = nullptr; void* stats = nullptr;
   size_t bytes = 0;
   // attend_bytes: of the attention's workspace
@@ -1877,7 +1877,6 @@ struct QuantSearch {
       c[l] = (float*)a.take(R * H * 4);
       cn[l] = (float*)a.take(R * H * 4);
     }
-    gates = (float*)a.take(R * 4 * H * 4);
     logits = (float*)a.take((size_t)R * cf.tgt_vocab * 4);
     stats = a.take(search_workspace(R, 1, cf.tgt_vocab));
     cache = a.take(CacheShape{B, 1, cf.hidden, S}.bytes());
@@ -1907,7 +1906,7 @@ int cmt_quant_decoder_pack(cmt_handle* h, int32_t group, void* weights_dev) {
   const int L = h->cfg.layers;
   for (int i = 0; i < L + 2; ++i) {
     const size_t off = i < L ? h->dec[i].w_off : i == L ? h->off_Wc : h->off_Wo;
-    launch_quant_pack(0, h->params + off, (size_t)q.shape[i].K, q.shape[i], (char*)weights_dev + q.at[i], h->st);
+    launch_quant_pack(0, h->params + off, (size_t)q.shape[i].K, q.shape[i], i < L, (char*)weights_dev + q.at[i], h->st);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(h, e, "cmt_quant_decoder_pack");
@@ -1965,32 +1964,30 @@ int cmt_quant_beam_decode(cmt_handle* h, int32_t group, const void* weights_dev,
     launch_beam_expand((int)esz, h->dec[l].Hst, h->dec[l].ph, h_in[l], (int)(l ? X : X0), R, R, K, H, st);
     launch_beam_expand(4, h->dec[l].Cst, H, s.c[l], H, R, R, K, H, st);
   }
-  auto job = [](const void* from, size_t from_pitch, void* to, size_t to_pitch, size_t bytes) {
-    return ReorderJob{(const char*)from, (char*)to, from_pitch, to_pitch, (int)bytes, 16};
+  // what a position takes over: the embeddings of the tokens, and the states and H_o of the hypotheses that they continue
+  auto job = [](const int32_t* rows, int src_rows, const void* from, size_t from_pitch, void* to, size_t to_pitch, size_t bytes) {
+    return ReorderJob{(const char*)from, (char*)to, from_pitch, to_pitch, rows, src_rows, (int)bytes, 16};
   };
-  ReorderJobs embed{}, follow{};
-  embed.job[0] = job(h->Pw(h->off_Etgt), E * esz, s.xcat, X0 * esz, E * esz);
+  ReorderJobs follow{};
   int n = 0;
-  follow.job[n++] = job(s.ho, H * esz, s.xcat + E * esz, X0 * esz, H * esz);
+  follow.job[n++] = job(bs.tok, V, h->Pw(h->off_Etgt), E * esz, s.xcat, X0 * esz, E * esz);
+  follow.job[n++] = job(bs.parent, R, s.ho, H * esz, s.xcat + E * esz, X0 * esz, H * esz);
   for (int l = 0; l < L; ++l) {
-    follow.job[n++] = job(s.hn[l], H * esz, h_in[l], (l ? X : X0) * esz, H * esz);
-    follow.job[n++] = job(s.cn[l], (size_t)H * 4, s.c[l], (size_t)H * 4, (size_t)H * 4);
+    follow.job[n++] = job(bs.parent, R, s.hn[l], H * esz, h_in[l], (l ? X : X0) * esz, H * esz);
+    follow.job[n++] = job(bs.parent, R, s.cn[l], (size_t)H * 4, s.c[l], (size_t)H * 4, (size_t)H * 4);
   }
   SearchAdvance adv{bs.hist_tok, bs.hist_par, bs.fin_step, bs.fin_par, bs.fin_tok, bs.fin_score, bs.hist_ld, 0, max_len, eos_id, length_penalty};
   for (int j = 0; j < max_len; ++j) {
-    launch_search_reorder(embed, 1, bs.tok, R, V, st);
-    for (int l = 0; l < L; ++l) {
-      launch_quant_product(p, l ? s.xl[l] : s.xcat, l ? X : X0, q.weight(l, weights_dev), R, h->params + h->dec[l].b_off, false, 0, s.gates, 4 * (size_t)H, st);
-      // the state goes to where the position's next layer (the last one's: the attentional layer) reads it
-      launch_quant_cell(p, s.gates, s.c[l], s.cn[l], s.hn[l], H, l + 1 < L ? s.xl[l + 1] : s.xc + H * esz, X, R, H, st);
-    }
+    launch_search_reorder(follow, j ? n : 1, R, st);   // (the first position: bos, and the states are there)
+    for (int l = 0; l < L; ++l)                       // the state also goes to where the next layer (of the last one: the attentional layer) reads it
+      launch_quant_lstm(p, l ? s.xl[l] : s.xcat, l ? X : X0, q.weight(l, weights_dev), R, h->params + h->dec[l].b_off, s.c[l], s.cn[l], s.hn[l], H,
+                        l + 1 < L ? s.xl[l + 1] : s.xc + H * esz, X, st);
     launch_cache_attend(p, shape, s.cache, s.hn[L - 1], H, K, 1, S, 1.f, s.xc, X, s.attend, st);
     launch_quant_product(p, s.xc, X, q.weight(L, weights_dev), R, nullptr, true, p, s.ho, H, st);
     launch_quant_product(p, s.ho, H, q.weight(L + 1, weights_dev), R, h->params + h->off_Bo, false, 0, s.logits, V, st);
     adv.j = j;
     launch_search_select(0, s.logits, V, bs.cum, B, K, V, K, bs.new_cum, bs.parent, bs.tok, &adv, s.stats, st);
     std::swap(bs.cum, bs.new_cum);                   // (both hold what one search needs: which is which does not matter afterwards)
-    if (j + 1 < max_len) launch_search_reorder(follow, n, bs.parent, R, R, st);
   }
   launch_beam_finish(bs, B, K, max_len, c.pad_id, out_ids_dev, out_len_dev, out_score_dev, st);
   (void)hipMemcpyAsync(h->h_flags, h->flags, sizeof(int), hipMemcpyDeviceToHost, st);

@@ -88,7 +88,7 @@ int cmt_quant_weight_pack(const void* weight_dev, int32_t type, int64_t pitch, i
   if (!type_ok(type)) return refuse("type must be CMT_FP32 or CMT_BF16");
   if (pitch < inputs) return refuse("pitch is less than inputs");
   if (misaligned(packed_dev, 256) || misaligned(weight_dev, type_size(type))) return refuse("packed weights are 256-byte aligned, others as their elements");
-  launch_quant_pack(type, weight_dev, (size_t)pitch, q, packed_dev, (hipStream_t)hip_stream);
+  launch_quant_pack(type, weight_dev, (size_t)pitch, q, false, packed_dev, (hipStream_t)hip_stream);
   return done("cmt_quant_weight_pack");
 }
 int cmt_quant_weight_encode(const uint8_t* codes_dev, const uint16_t* scales_dev, int32_t outputs, int32_t inputs, int32_t group, void* packed_dev,
@@ -237,10 +237,10 @@ int cmt_beam_reorder(const int32_t* rows_dev, int32_t count, int32_t source_rows
     for (int i = 0; i < m; ++i) {
       const cmt_reorder_tensor& a = tensors[i0 + i];
       const uint64_t bits = (uintptr_t)a.source_dev | (uintptr_t)a.target_dev | (uint64_t)a.source_pitch | (uint64_t)a.target_pitch | (uint64_t)a.row_bytes;
-      jobs.job[i] = ReorderJob{(const char*)a.source_dev, (char*)a.target_dev, (size_t)a.source_pitch, (size_t)a.target_pitch, (int)a.row_bytes,
+      jobs.job[i] = ReorderJob{(const char*)a.source_dev, (char*)a.target_dev, (size_t)a.source_pitch, (size_t)a.target_pitch, rows_dev, source_rows, (int)a.row_bytes,
                                bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : bits % 2 == 0 ? 2 : 1};
     }
-    launch_search_reorder(jobs, m, rows_dev, count, source_rows, (hipStream_t)hip_stream);
+    launch_search_reorder(jobs, m, count, (hipStream_t)hip_stream);
   }
   return done("cmt_beam_reorder");
 }

@@ -23,15 +23,17 @@ struct QuantShape {
   size_t bytes() const { return (code_bytes() + scale_bytes() + 255) & ~(size_t)255; }
 };
 struct QuantWeightRef { QuantShape shape; const char* packed; };
-void launch_quant_pack(int prec, const void* w, size_t ldw, const QuantShape& q, void* packed, hipStream_t st);
+// gates: an LSTM layer's weight (blocks of N / 4 rows i, f, g, o), packed with a unit's four rows side by side.
+void launch_quant_pack(int prec, const void* w, size_t ldw, const QuantShape& q, bool gates, void* packed, hipStream_t st);
 void launch_quant_encode(const uint8_t* codes, const bf16_t* scales, const QuantShape& q, void* packed, hipStream_t st);
 void launch_quant_values(const void* packed, const QuantShape& q, float* out, hipStream_t st);
 // y [M, N] = f(x [M, K] W^T + bias), f = tanh or nothing; x of type prec, y of type y_prec; bias fp32 or null.
 void launch_quant_product(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, bool tanh, int y_prec, void* y,
                           size_t ldy, hipStream_t st);
-// The cell of an LSTM step: gates [R, 4 H] fp32 (blocks i, f, g, o, before their nonlinearities), c_prev [R, H] -> c [R, H] fp32 and the state
-// in type prec to two places (h2 may be null; pitches in elements).  H and the pitches are multiples of 4, as are the addresses in elements.
-void launch_quant_cell(int prec, const float* gates, const float* c_prev, float* c, void* h, size_t ldh, void* h2, size_t ldh2, int R, int H, hipStream_t st);
+// An LSTM layer's position: the gates x W^T + bias (W packed as gates; bias in blocks i, f, g, o of H) and their cells, c_prev [M, H] -> c [M, H]
+// fp32 and the state in type prec to two places (pitches in elements).
+void launch_quant_lstm(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, const float* c_prev, float* c, void* h,
+                       size_t ldh, void* h2, size_t ldh2, hipStream_t st);
 
 // ---- cache.hip: source rows in 8 bits -------------------------------------------------------------
 // Per (sequence, head, block of 32 tokens) one fp32 scale for the keys and one for the values; codes are whole numbers -127..127.
@@ -82,9 +84,9 @@ size_t search_workspace(int B, int K, int V);
 void launch_search_select(int prec, const void* logits, size_t ld, const float* scores, int B, int K, int V, int n, float* out_scores,
                           int32_t* out_rows, int32_t* out_tokens, const SearchAdvance* adv, void* workspace, hipStream_t st);
 constexpr int REORDER_MAX = 32;
-struct ReorderJob { const char* src; char* dst; size_t src_pitch, dst_pitch; int bytes, step; };   // step: 16, 8, 4, 2 or 1 bytes at a time
+struct ReorderJob { const char* src; char* dst; size_t src_pitch, dst_pitch; const int32_t* rows; int src_rows, bytes, step; };   // step: 16, 4, 2 or 1 bytes at a time
 struct ReorderJobs { ReorderJob job[REORDER_MAX]; };
-void launch_search_reorder(const ReorderJobs& jobs, int n, const int32_t* rows, int count, int src_rows, hipStream_t st);
+void launch_search_reorder(const ReorderJobs& jobs, int n, int count, hipStream_t st);
 
 // ---- shared ------------------------------------------------------------------------------------------
 // Over the 16 lanes of a row, in every lane, by DPP moves (a shuffle through LDS is ten times as long).

@@ -24,18 +24,19 @@ __device__ __forceinline__ size_t quant_dword(int n, int k, int k_tiles) {   // 
 // One thread per 8 weights; the threads of a group are neighbours.  scale = bf16(max|w| / 6), code = the nearest one (the even one of two);
 // a group with a weight that is no finite number has the scale NaN, so that no product hides it.
 template <typename T>
-__global__ __launch_bounds__(256) void quant_pack_kernel(const T* __restrict__ w, size_t ldw, QuantShape q, int k_tiles, int row_blocks,
+__global__ __launch_bounds__(256) void quant_pack_kernel(const T* __restrict__ w, size_t ldw, QuantShape q, int gates, int k_tiles, int row_blocks,
                                                          uint32_t* __restrict__ codes, bf16_t* __restrict__ scales) {
   const int per_row = k_tiles * (QUANT_TILE_K / 8), share = q.group / 8;
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
   const size_t n = i / per_row;                              // (per_row is a multiple of 16: a group's threads are in one row)
   const int k = (int)(i - n * per_row) * 8;
   if (n >= (size_t)row_blocks * 16) return;
+  const size_t from = gates ? (n & 3) * (q.N >> 2) + (n >> 2) : n;
   float x[8], most = 0.f;
   bool bad = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    x[e] = n < (size_t)q.N && k + e < q.K ? to_f(w[n * ldw + k + e]) : 0.f;
+    x[e] = n < (size_t)q.N && k + e < q.K ? to_f(w[from * ldw + k + e]) : 0.f;
     bad |= !(fabsf(x[e]) <= 3.4028235e38f);
     most = fmaxf(most, fabsf(x[e]));
   }
@@ -55,14 +56,14 @@ __global__ __launch_bounds__(256) void quant_pack_kernel(const T* __restrict__ w
   codes[quant_dword((int)n, k, k_tiles)] = word;
   if (k % q.group == 0) scales[((n >> 4) * (size_t)k_tiles * (QUANT_TILE_K / q.group) + k / q.group) * 16 + (n & 15)] = sb;
 }
-void launch_quant_pack(int prec, const void* w, size_t ldw, const QuantShape& q, void* packed, hipStream_t st) {
+void launch_quant_pack(int prec, const void* w, size_t ldw, const QuantShape& q, bool gates, void* packed, hipStream_t st) {
   const size_t threads = (size_t)q.row_blocks() * 16 * q.k_tiles() * (QUANT_TILE_K / 8);
   const dim3 grid((unsigned)((threads + 255) / 256));
   bf16_t* scales = (bf16_t*)((char*)packed + q.code_bytes());
   if (prec)
-    hipLaunchKernelGGL(quant_pack_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t*)w, ldw, q, q.k_tiles(), q.row_blocks(), (uint32_t*)packed, scales);
+    hipLaunchKernelGGL(quant_pack_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t*)w, ldw, q, gates, q.k_tiles(), q.row_blocks(), (uint32_t*)packed, scales);
   else
-    hipLaunchKernelGGL(quant_pack_kernel<float>, grid, dim3(256), 0, st, (const float*)w, ldw, q, q.k_tiles(), q.row_blocks(), (uint32_t*)packed, scales);
+    hipLaunchKernelGGL(quant_pack_kernel<float>, grid, dim3(256), 0, st, (const float*)w, ldw, q, gates, q.k_tiles(), q.row_blocks(), (uint32_t*)packed, scales);
 }
 // codes [N, K] one to a byte (the lower four bits count), scales [N, ceil(K / group)]
 __global__ __launch_bounds__(256) void quant_encode_kernel(const uint8_t* __restrict__ src, const bf16_t* __restrict__ src_scales, QuantShape q,
@@ -105,9 +106,24 @@ void launch_quant_values(const void* packed, const QuantShape& q, float* out, hi
                      (const bf16_t*)((const char*)packed + q.code_bytes()), q, q.k_tiles(), out);
 }
 
-// four neighbouring outputs of row m; flags: 1 tanh, 2 y in bf16, 8 y takes them in one piece
+// Four neighbouring outputs of row m; flags: 1 tanh, 2 y in bf16, 8 y takes them in one piece, 16 they are the gates of an LSTM's unit.
+// An LSTM layer's weight is packed with a unit's four gates side by side, so that the lane that ends up with them makes the unit's cell: no
+// gates in memory and no launch for the cells (10 rows, width 1024: 5.0 us a layer against 4.4 + 2.6; 640 rows 38 against 37 + 5).
+struct QuantCell { const float* c_prev; float* c; void *h, *h2; size_t ldh, ldh2; };
+template <typename T>
 __device__ __forceinline__ void quant_store(float a, float b, float c, float d, int m, int n, int N, const float* __restrict__ bias, int flags,
-                                            void* __restrict__ y, size_t ldy) {
+                                            void* __restrict__ y, size_t ldy, const QuantCell& cell) {
+  if (flags & 16) {
+    constexpr bool FAST = sizeof(T) == 2;
+    const int H = N >> 2, u = n >> 2;
+    const float in = sigm_of<FAST>(a + bias[u]), forget = sigm_of<FAST>(b + bias[H + u]), out = sigm_of<FAST>(d + bias[3 * H + u]);
+    const float x = forget * cell.c_prev[(size_t)m * H + u] + in * tanh_of<FAST>(c + bias[2 * H + u]);
+    const T h = from_f<T>(out * tanh_of<FAST>(x));
+    cell.c[(size_t)m * H + u] = x;
+    ((T*)cell.h)[m * cell.ldh + u] = h;
+    ((T*)cell.h2)[m * cell.ldh2 + u] = h;
+    return;
+  }
   float r[4] = {a, b, c, d};
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -135,7 +151,7 @@ template <typename T, int GROUP, int NT, int CT, bool WHOLE>
 __global__ __launch_bounds__(64 * QUANT_WAVES) void quant_product_kernel(const T* __restrict__ x, size_t ldx, const uint4* __restrict__ codes,
                                                                          const bf16_t* __restrict__ scales, int M, int N, int K, int k_tiles,
                                                                          int row_blocks, int m_blocks, const float* __restrict__ bias, int flags,
-                                                                         void* __restrict__ y, size_t ldy) {
+                                                                         void* __restrict__ y, size_t ldy, QuantCell cell) {
   constexpr int PARTS = OPERAND_PARTS<T>, PER = QUANT_TILE_K / GROUP, STEPS = GROUP / 32;
   __shared__ float4 red[QUANT_WAVES][NT * CT][64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -214,7 +230,7 @@ __global__ __launch_bounds__(64 * QUANT_WAVES) void quant_product_kernel(const T
     }
     const int m = m0 + 16 * (t % CT) + (l & 15), n = (nb + t / CT) * 16 + 4 * (l >> 4);
     if (m >= M || n >= N) continue;
-    quant_store(v.x, v.y, v.z, v.w, m, n, N, bias, flags, y, ldy);
+    quant_store<T>(v.x, v.y, v.z, v.w, m, n, N, bias, flags, y, ldy, cell);
   }
 }
 
@@ -227,7 +243,7 @@ template <typename T, int GROUP, int MT, bool WHOLE>
 __global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T* __restrict__ x, size_t ldx, const uint4* __restrict__ codes,
                                                                  const bf16_t* __restrict__ scales, int M, int N, int K, int k_tiles, int row_blocks,
                                                                  int m_blocks, const float* __restrict__ bias, int flags, void* __restrict__ y,
-                                                                 size_t ldy) {
+                                                                 size_t ldy, QuantCell cell) {
   constexpr int PARTS = OPERAND_PARTS<T>, PER = QUANT_TILE_K / GROUP, STEPS = GROUP / 32, WN = 4, NT = 4;
   constexpr bool DIRECT = WHOLE && sizeof(T) == 2;
   constexpr int THREADS = QUANT_WIDE, SLOTS = 2 * MT * 4 * 64, MINE = SLOTS / THREADS;
@@ -369,28 +385,29 @@ __global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T*
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
       const int m = m0 + 16 * (wm * MT + j) + c;
-      if (m < M) quant_store(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], m, n, N, bias, flags, y, ldy);
+      if (m < M) quant_store<T>(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], m, n, N, bias, flags, y, ldy, cell);
     }
   }
 }
 
 template <typename T, int GROUP, int NT, int CT>
-static void quant_product_go(const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, int flags, void* y, size_t ldy, hipStream_t st) {
+static void quant_product_go(const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, int flags, void* y, size_t ldy, const QuantCell& cell,
+                             hipStream_t st) {
   const QuantShape& q = w.shape;
   const int m_blocks = (M + 16 * CT - 1) / (16 * CT);
   const int n_blocks = ((q.row_blocks() + NT - 1) / NT + 7) / 8 * 8;
   auto* kernel = flags & 4 ? quant_product_kernel<T, GROUP, NT, CT, true> : quant_product_kernel<T, GROUP, NT, CT, false>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)n_blocks * m_blocks), dim3(64 * QUANT_WAVES), 0, st, (const T*)x, ldx, (const uint4*)w.packed,
-                     (const bf16_t*)(w.packed + q.code_bytes()), M, q.N, q.K, q.k_tiles(), q.row_blocks(), m_blocks, bias, flags, y, ldy);
+                     (const bf16_t*)(w.packed + q.code_bytes()), M, q.N, q.K, q.k_tiles(), q.row_blocks(), m_blocks, bias, flags, y, ldy, cell);
 }
 template <typename T, int GROUP, int MT>
 static void quant_product_wide_go(const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, int flags, void* y, size_t ldy,
-                                  hipStream_t st) {
+                                  const QuantCell& cell, hipStream_t st) {
   const QuantShape& q = w.shape;
   const int m_blocks = (M + 32 * MT - 1) / (32 * MT), n_blocks = ((q.row_blocks() + 15) / 16 + 7) / 8 * 8;
   auto* kernel = flags & 4 ? quant_product_wide_kernel<T, GROUP, MT, true> : quant_product_wide_kernel<T, GROUP, MT, false>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)n_blocks * m_blocks), dim3(QUANT_WIDE), 0, st, (const T*)x, ldx, (const uint4*)w.packed,
-                     (const bf16_t*)(w.packed + q.code_bytes()), M, q.N, q.K, q.k_tiles(), q.row_blocks(), m_blocks, bias, flags, y, ldy);
+                     (const bf16_t*)(w.packed + q.code_bytes()), M, q.N, q.K, q.k_tiles(), q.row_blocks(), m_blocks, bias, flags, y, ldy, cell);
 }
 // Which kernel and tile, by sizes alone; times are of whole calls, us, 11 of them the host's (bf16 unless said).
 //   Many rows: k is not split there, so it takes workgroups of 64 rows for most of the chip.  32000 x 1024, groups of 128 | 32: 64 rows
@@ -402,67 +419,45 @@ static void quant_product_wide_go(const void* x, size_t ldx, const QuantWeightRe
 //   11 against 18; 512 x 4096 in fp32, 128 rows 17 against 12).
 template <typename T, int GROUP>
 static void quant_product_tiles(const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, int flags, void* y, size_t ldy,
-                                hipStream_t st) {
+                                const QuantCell& cell, hipStream_t st) {
   constexpr int MOST = sizeof(T) == 4 || GROUP == 32 ? 2 : GROUP == 64 ? 4 : 5, CT = sizeof(T) == 4 ? 1 : 2;
   const long rb = w.shape.row_blocks();
   auto wgs = [&](int mt) { return (rb + 15) / 16 * ((M + 32 * mt - 1) / (32 * mt)); };
   if (M > 64 && wgs(2) >= 200) {
     if constexpr (MOST > 2)
-      if ((wgs(MOST) + 255) / 256 * (MOST + 1) <= (wgs(2) + 255) / 256 * 3) { quant_product_wide_go<T, GROUP, MOST>(x, ldx, w, M, bias, flags, y, ldy, st); return; }
-    quant_product_wide_go<T, GROUP, 2>(x, ldx, w, M, bias, flags, y, ldy, st);
+      if ((wgs(MOST) + 255) / 256 * (MOST + 1) <= (wgs(2) + 255) / 256 * 3) { quant_product_wide_go<T, GROUP, MOST>(x, ldx, w, M, bias, flags, y, ldy, cell, st); return; }
+    quant_product_wide_go<T, GROUP, 2>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
     return;
   }
   if constexpr (CT > 1)
     if (M > 16) {
-      if (rb * ((M + 31) / 32) < 512) quant_product_go<T, GROUP, 1, CT>(x, ldx, w, M, bias, flags, y, ldy, st);
-      else quant_product_go<T, GROUP, 4, CT>(x, ldx, w, M, bias, flags, y, ldy, st);
+      if (rb * ((M + 31) / 32) < 512) quant_product_go<T, GROUP, 1, CT>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
+      else quant_product_go<T, GROUP, 4, CT>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
       return;
     }
-  if (rb * ((M + 15) / 16) < 512) quant_product_go<T, GROUP, 1, 1>(x, ldx, w, M, bias, flags, y, ldy, st);
-  else quant_product_go<T, GROUP, 4, 1>(x, ldx, w, M, bias, flags, y, ldy, st);
+  if (rb * ((M + 15) / 16) < 512) quant_product_go<T, GROUP, 1, 1>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
+  else quant_product_go<T, GROUP, 4, 1>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
 }
-void launch_quant_product(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, bool tanh, int y_prec, void* y,
-                          size_t ldy, hipStream_t st) {
-  const size_t xs = prec ? 2 : 4, ys = y_prec ? 2 : 4;
-  const int flags = (tanh ? 1 : 0) | (y_prec ? 2 : 0) | (((uintptr_t)x | ldx * xs) % 16 == 0 && w.shape.K % 8 == 0 && ldx <= 1 << 20 ? 4 : 0) | (((uintptr_t)y | ldy * ys) % (4 * ys) == 0 ? 8 : 0);
+static void quant_product_any(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, int flags, void* y, size_t ldy,
+                              const QuantCell& cell, hipStream_t st) {
+  if (((uintptr_t)x | ldx * (prec ? 2 : 4)) % 16 == 0 && w.shape.K % 8 == 0 && ldx <= 1 << 20) flags |= 4;
   auto go = [&](auto type) {
     using T = decltype(type);
-    if (w.shape.group == 32) quant_product_tiles<T, 32>(x, ldx, w, M, bias, flags, y, ldy, st);
-    else if (w.shape.group == 64) quant_product_tiles<T, 64>(x, ldx, w, M, bias, flags, y, ldy, st);
-    else quant_product_tiles<T, 128>(x, ldx, w, M, bias, flags, y, ldy, st);
+    if (w.shape.group == 32) quant_product_tiles<T, 32>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
+    else if (w.shape.group == 64) quant_product_tiles<T, 64>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
+    else quant_product_tiles<T, 128>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
   };
   if (prec) go(bf16_t{}); else go(float{});
 }
-
-// ---- the cell behind a layer's product ----------------------------------------------------------------------
-template <typename T>
-__global__ __launch_bounds__(256) void quant_cell_kernel(const float* __restrict__ gates, const float* __restrict__ c_prev, float* __restrict__ c,
-                                                         T* __restrict__ h, size_t ldh, T* __restrict__ h2, size_t ldh2, int R, int H) {
-  constexpr bool FAST = sizeof(T) == 2;
-  const int per = H >> 2, i = blockIdx.x * 256 + threadIdx.x, r = i / per, u = (i - r * per) * 4;
-  if (r >= R) return;
-  const float* g = gates + (size_t)r * 4 * H + u;
-  const float4 gi = *reinterpret_cast<const float4*>(g), gf = *reinterpret_cast<const float4*>(g + H);
-  const float4 gg = *reinterpret_cast<const float4*>(g + 2 * H), go = *reinterpret_cast<const float4*>(g + 3 * H);
-  const float4 cp = *reinterpret_cast<const float4*>(c_prev + (size_t)r * H + u);
-  float4 cn;
-  T hn[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float x = sigm_of<FAST>((&gf.x)[e]) * (&cp.x)[e] + sigm_of<FAST>((&gi.x)[e]) * tanh_of<FAST>((&gg.x)[e]);
-    (&cn.x)[e] = x;
-    hn[e] = from_f<T>(sigm_of<FAST>((&go.x)[e]) * tanh_of<FAST>(x));
-  }
-  *reinterpret_cast<float4*>(c + (size_t)r * H + u) = cn;
-  struct alignas(4 * sizeof(T)) Four { T v[4]; };
-  const Four f{{hn[0], hn[1], hn[2], hn[3]}};
-  *reinterpret_cast<Four*>(h + r * ldh + u) = f;
-  if (h2) *reinterpret_cast<Four*>(h2 + r * ldh2 + u) = f;
+void launch_quant_product(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, bool tanh, int y_prec, void* y,
+                          size_t ldy, hipStream_t st) {
+  const size_t ys = y_prec ? 2 : 4;
+  const int flags = (tanh ? 1 : 0) | (y_prec ? 2 : 0) | (((uintptr_t)y | ldy * ys) % (4 * ys) == 0 ? 8 : 0);
+  quant_product_any(prec, x, ldx, w, M, bias, flags, y, ldy, QuantCell{}, st);
 }
-void launch_quant_cell(int prec, const float* gates, const float* c_prev, float* c, void* h, size_t ldh, void* h2, size_t ldh2, int R, int H, hipStream_t st) {
-  const dim3 grid((unsigned)(((size_t)R * (H / 4) + 255) / 256));
-  if (prec) hipLaunchKernelGGL(quant_cell_kernel<bf16_t>, grid, dim3(256), 0, st, gates, c_prev, c, (bf16_t*)h, ldh, (bf16_t*)h2, ldh2, R, H);
-  else hipLaunchKernelGGL(quant_cell_kernel<float>, grid, dim3(256), 0, st, gates, c_prev, c, (float*)h, ldh, (float*)h2, ldh2, R, H);
+void launch_quant_lstm(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, const float* c_prev, float* c, void* h,
+                       size_t ldh, void* h2, size_t ldh2, hipStream_t st) {
+  quant_product_any(prec, x, ldx, w, M, bias, 16, nullptr, 0, QuantCell{c_prev, c, h, h2, ldh, ldh2}, st);
 }
 
 }  // namespace cmt

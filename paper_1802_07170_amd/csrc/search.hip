@@ -285,10 +285,10 @@ template <typename V>
 __device__ __forceinline__ void reorder_row(const char* s, char* d, int bytes) {
   for (int i = threadIdx.x; i < bytes / (int)sizeof(V); i += 128) reinterpret_cast<V*>(d)[i] = reinterpret_cast<const V*>(s)[i];
 }
-__global__ __launch_bounds__(128) void search_reorder_kernel(ReorderJobs jobs, const int32_t* __restrict__ rows, int src_rows) {
-  const int r = blockIdx.x, from = rows[r];
-  if ((unsigned)from >= (unsigned)src_rows) return;
+__global__ __launch_bounds__(128) void search_reorder_kernel(ReorderJobs jobs) {
   const ReorderJob& j = jobs.job[blockIdx.y];
+  const int r = blockIdx.x, from = j.rows[r];
+  if ((unsigned)from >= (unsigned)j.src_rows) return;
   const char* s = j.src + (size_t)from * j.src_pitch;
   char* d = j.dst + (size_t)r * j.dst_pitch;
   if (j.step == 16) reorder_row<uint4>(s, d, j.bytes);
@@ -296,8 +296,8 @@ __global__ __launch_bounds__(128) void search_reorder_kernel(ReorderJobs jobs, c
   else if (j.step == 2) reorder_row<uint16_t>(s, d, j.bytes);
   else reorder_row<uint8_t>(s, d, j.bytes);
 }
-void launch_search_reorder(const ReorderJobs& jobs, int n, const int32_t* rows, int count, int src_rows, hipStream_t st) {
-  hipLaunchKernelGGL(search_reorder_kernel, dim3(count, n), dim3(128), 0, st, jobs, rows, src_rows);
+void launch_search_reorder(const ReorderJobs& jobs, int n, int count, hipStream_t st) {
+  hipLaunchKernelGGL(search_reorder_kernel, dim3(count, n), dim3(128), 0, st, jobs);
 }
 
 }  // namespace cmt
