@@ -275,7 +275,7 @@ const char* cmt_operator_error(void);
  *   cmt_quant_weight_pack    from a weight (row-major, pitch in elements): scale = bf16(max|w| / 6), the nearest codes (of two as near the
  *                            even one).  A group with a value that is not finite gets the scale NaN, so that its products are NaN;
  *   cmt_quant_weight_encode  from codes (row-major, one to a byte, the upper four bits ignored) and bf16 scales [outputs, ceil(inputs / group)];
- * and cmt_quant_weight_values gives W in fp32, row-major.  1 <= outputs <= 2^24, 1 <= inputs <= 2^16, outputs * inputs <= 2^36. */
+ * and cmt_quant_weight_values gives W in fp32, row-major.  1 <= outputs <= 2^24, 1 <= inputs <= 2^16, outputs * inputs <= 2^34. */
 int cmt_quant_weight_bytes(int32_t outputs, int32_t inputs, int32_t group, size_t* bytes);
 int cmt_quant_weight_pack(const void* weight_dev, int32_t type, int64_t pitch, int32_t outputs, int32_t inputs, int32_t group, void* packed_dev,
                           void* hip_stream);
@@ -283,7 +283,7 @@ int cmt_quant_weight_encode(const uint8_t* codes_dev, const uint16_t* scales_dev
                             void* hip_stream);
 int cmt_quant_weight_values(const void* packed_dev, int32_t outputs, int32_t inputs, int32_t group, float* weight_dev, void* hip_stream);
 /* y[m, n] = f(sum_k x[m, k] W[n, k] + bias[n]), f = tanh where tanh_of is not 0; bias_dev (fp32) may be NULL.  x of `type`, y of y_type (CMT_FP32
- * or CMT_BF16), row-major with pitches in elements; 0 <= rows <= 65535 (0: nothing is done); y shares no memory with x.  Products are exact, sums fp32 in either
+ * or CMT_BF16), row-major with pitches in elements; 0 <= rows <= 65535 (0: nothing is done), outputs * rows <= 2^36; y shares no memory with x.  Products are exact, sums fp32 in either
  * type, in an order that the sizes alone decide. */
 int cmt_quant_product(const void* x_dev, int32_t type, int64_t x_pitch, int32_t rows, const void* packed_dev, int32_t outputs, int32_t inputs,
                       int32_t group, const float* bias_dev, int32_t tanh_of, void* y_dev, int32_t y_type, int64_t y_pitch, void* hip_stream);
@@ -313,17 +313,18 @@ int cmt_cache_attend(const cmt_cache_config* cache, const void* cache_dev, const
  * best first, of equal ones the lower (s, v).  logits of `type`, [sentences * beam, vocab] with a pitch in elements; scores fp32
  * [sentences, beam], -inf for a place without a hypothesis (its logits are not read).  A logit of -inf is never taken; a row with a logit that
  * is NaN or +inf, or whose score is no finite number, has no extensions.  Out, [sentences, n]: the scores in fp32, the row b * beam + s that is
- * extended and the token; -inf, -1, -1 where there are fewer than n.  beam, n <= 32, vocab <= 2^26.  Scores are compared in 64 bits. */
+ * extended and the token; -inf, -1, -1 where there are fewer than n.  beam, n <= 32, vocab <= 2^26, sentences * beam *
+ * ceil(vocab / 512) <= 2^25.  Scores are compared in 64 bits. */
 int cmt_beam_select_workspace(int32_t sentences, int32_t beam, int32_t vocab, size_t* bytes);
 int cmt_beam_select(const void* logits_dev, int32_t type, int64_t pitch, const float* scores_dev, int32_t sentences, int32_t beam, int32_t vocab,
                     int32_t n, float* out_scores_dev, int32_t* out_rows_dev, int32_t* out_tokens_dev, void* workspace_dev, size_t workspace_bytes,
                     void* hip_stream);
-/* target[r] = source[rows[r]] for r < count, of n <= 256 tensors of rows of row_bytes (pitches in bytes; `tensors` is host memory, read before the call
- * returns).  A row whose number is outside [0, source_rows) is left as it was.  No target may overlap a source or another target. */
+/* target[r] = source[rows[r]] for r < count <= 2^24, of n <= 256 tensors of rows of row_bytes (pitches in bytes; `tensors` is host memory, read before the call
+ * returns).  A row whose number is outside [0, source_rows) is left as it was.  No target may overlap a source, another target or rows. */
 typedef struct cmt_reorder_tensor { const void* source_dev; void* target_dev; int64_t source_pitch, target_pitch, row_bytes; } cmt_reorder_tensor;
 int cmt_beam_reorder(const int32_t* rows_dev, int32_t count, int32_t source_rows, const cmt_reorder_tensor* tensors, int32_t n, void* hip_stream);
 /* The decoder of a handle in small numbers: cmt_beam_decode with the weights of the decoder's layers, of W_c and of the output layer in
- * 4 bits (a fifth of the 16-bit ones' bytes, with groups of 64) and the source rows (keys W_a^T H_s and states H_s) in 8.  Biases, embeddings, the encoder, states, cells and scores are as in
+ * 4 bits (4.25 bits a weight with groups of 64) and the source rows (keys W_a^T H_s and states H_s) in 8.  Biases, embeddings, the encoder, states, cells and scores are as in
  * cmt_beam_decode, and so are the arguments, the search's rules and the errors.
  *   cmt_quant_decoder_bytes  of the packed weights and of the workspace of a search (any B, S and beam that the configuration allows);
  *   cmt_quant_decoder_pack   writes the packed weights from the handle's parameters as they are (enqueued; again after they change);

@@ -43,7 +43,7 @@ bool overlap(const Rows& a, const Rows& b) {
 
 bool quant_shape(int32_t outputs, int32_t inputs, int32_t group, QuantShape* q) {
   if (outputs < 1 || outputs > 1 << 24 || inputs < 1 || inputs > 1 << 16) { refuse("outputs must be in [1, 2^24], inputs in [1, 2^16]"); return false; }
-  if ((int64_t)outputs * inputs > (int64_t)1 << 36) { refuse("outputs * inputs must be at most 2^36"); return false; }
+  if ((int64_t)outputs * inputs > (int64_t)1 << 34) { refuse("outputs * inputs must be at most 2^34"); return false; }   // (a grid has less than 2^32 threads)
   if (group != 32 && group != 64 && group != 128) { refuse("group must be 32, 64 or 128"); return false; }
   *q = QuantShape{outputs, inputs, group};
   return true;
@@ -113,7 +113,7 @@ int cmt_quant_product(const void* x_dev, int32_t type, int64_t x_pitch, int32_t 
   QuantShape q;
   if (!quant_shape(outputs, inputs, group, &q)) return CMT_EINVAL;
   if (!type_ok(type) || !type_ok(y_type)) return refuse("types must be CMT_FP32 or CMT_BF16");
-  if (rows < 0 || rows > 65535 || (int64_t)q.row_blocks() * ((rows + 15) / 16) > 1 << 30) return refuse("rows must be in [0, 65535], outputs * rows at most 2^38");
+  if (rows < 0 || rows > 65535 || (int64_t)q.row_blocks() * ((rows + 15) / 16) > 1 << 28) return refuse("rows must be in [0, 65535], outputs * rows at most 2^36");
   if (rows == 0) return CMT_OK;
   if (!x_dev || !packed_dev || !y_dev) return refuse("null pointer");
   if (x_pitch < inputs || y_pitch < outputs) return refuse("a pitch is less than its row");
@@ -186,7 +186,7 @@ static bool select_shape(int32_t sentences, int32_t beam, int32_t vocab, int32_t
   if (sentences < 1 || sentences > 1 << 20) { refuse("sentences must be in [1, 2^20]"); return false; }
   if (beam < 1 || beam > SEARCH_MAX || n < 1 || n > SEARCH_MAX) { refuse("beam and n must be in [1, %d]", SEARCH_MAX); return false; }
   if (vocab < 1 || vocab > SEARCH_MAX_VOCAB) { refuse("vocab must be in [1, %d]", SEARCH_MAX_VOCAB); return false; }
-  if ((double)sentences * beam * ((vocab + SEARCH_GROUP - 1) / SEARCH_GROUP) > 1e9) { refuse("more than 10^9 groups of logits"); return false; }
+  if ((double)sentences * beam * ((vocab + SEARCH_GROUP - 1) / SEARCH_GROUP) > 1 << 25) { refuse("more than 2^25 groups of %d logits", SEARCH_GROUP); return false; }
   return true;
 }
 int cmt_beam_select_workspace(int32_t sentences, int32_t beam, int32_t vocab, size_t* bytes) {
@@ -212,7 +212,7 @@ int cmt_beam_select(const void* logits_dev, int32_t type, int64_t pitch, const f
   return done("cmt_beam_select");
 }
 int cmt_beam_reorder(const int32_t* rows_dev, int32_t count, int32_t source_rows, const cmt_reorder_tensor* tensors, int32_t n, void* hip_stream) {
-  if (n < 0 || n > 256 || count < 0 || source_rows < 0) return refuse("counts must not be negative, tensors at most 256");
+  if (n < 0 || n > 256 || count < 0 || count > 1 << 24 || source_rows < 0) return refuse("counts must not be negative, tensors at most 256, rows at most 2^24");
   if (n == 0 || count == 0) return CMT_OK;
   if (!rows_dev || !tensors) return refuse("null pointer");
   if (misaligned(rows_dev, 4)) return refuse("rows are 4-byte aligned");
@@ -230,6 +230,7 @@ int cmt_beam_reorder(const int32_t* rows_dev, int32_t count, int32_t source_rows
         return refuse("the target of tensor %d overlaps the source of tensor %d", i, k);
       if (k < i && overlap(target, Rows{(uintptr_t)b.target_dev, (uint64_t)b.target_pitch, (uint64_t)b.row_bytes, (uint64_t)count}))
         return refuse("the targets of tensors %d and %d overlap", k, i);
+      if (k == i && overlap(target, Rows{(uintptr_t)rows_dev, (uint64_t)count * 4, (uint64_t)count * 4, 1})) return refuse("the target of tensor %d overlaps the rows' numbers", i);
     }
   for (int i0 = 0; i0 < n; i0 += REORDER_MAX) {
     ReorderJobs jobs{};

@@ -88,21 +88,19 @@ void launch_quant_encode(const uint8_t* codes, const bf16_t* scales, const Quant
   hipLaunchKernelGGL(quant_encode_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, codes, scales, q, q.k_tiles(), q.row_blocks(),
                      (uint32_t*)packed, (bf16_t*)((char*)packed + q.code_bytes()));
 }
-__global__ __launch_bounds__(256) void quant_values_kernel(const uint32_t* __restrict__ codes, const bf16_t* __restrict__ scales, QuantShape q,
+__global__ __launch_bounds__(128) void quant_values_kernel(const uint32_t* __restrict__ codes, const bf16_t* __restrict__ scales, QuantShape q,
                                                            int k_tiles, float* __restrict__ out) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (size_t)q.N * q.K) return;
-  const size_t n = i / q.K;
-  const int k = (int)(i - n * q.K);
+  const size_t n = blockIdx.x;
+  const int k = blockIdx.y * 128 + threadIdx.x;
+  if (k >= q.K) return;
   const uint32_t c = codes[quant_dword((int)n, k & ~7, k_tiles)] >> (4 * (k & 7)) & 15;
   const uint32_t e = c & 7;                                  // two exponent bits, one of the mantissa
   const float size = e < 2 ? 0.5f * e : (1.0f + 0.5f * (e & 1)) * (float)(1 << ((e >> 1) - 1));
   const float s = bf2f(scales[((n >> 4) * (size_t)k_tiles * (QUANT_TILE_K / q.group) + k / q.group) * 16 + (n & 15)]);
-  out[i] = (c & 8 ? -size : size) * s;
+  out[n * q.K + k] = (c & 8 ? -size : size) * s;
 }
 void launch_quant_values(const void* packed, const QuantShape& q, float* out, hipStream_t st) {
-  const size_t n = (size_t)q.N * q.K;
-  hipLaunchKernelGGL(quant_values_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (const uint32_t*)packed,
+  hipLaunchKernelGGL(quant_values_kernel, dim3(q.N, q.k_tiles()), dim3(128), 0, st, (const uint32_t*)packed,
                      (const bf16_t*)((const char*)packed + q.code_bytes()), q, q.k_tiles(), out);
 }
 

@@ -308,6 +308,8 @@ class QuantDecoder:
         """As Trainer.beam_decode: ids [B, max_len], lengths [B], normalised scores [B] (numpy)."""
         tr = self.trainer
         src, lens = (torch.from_numpy(np.ascontiguousarray(a, np.int32)).to(tr.device) for a in (src_ids, src_len))
+        if src.dim() != 2 or tuple(lens.shape) != src.shape[:1]:
+            raise ValueError(f"src_ids must be [B, S] and src_len [B], not {tuple(src.shape)} and {tuple(lens.shape)}")
         B, S = src.shape
         out = torch.empty((B, max_len), dtype=torch.int32, device=tr.device)
         length = torch.empty((B,), dtype=torch.int32, device=tr.device)

@@ -95,3 +95,21 @@ def test_tensors_off_the_device_are_refused():
                  lambda: decoding.beam_reorder(torch.zeros(2, dtype=torch.int32), [x], [x])):
         with pytest.raises(ValueError):
             call()
+
+
+def test_more_than_a_launch_can_count(lib):
+    """Grids of 2^32 threads and more are refused as arguments, not by the launch."""
+    n = C.c_size_t()
+    assert lib.cmt_quant_weight_bytes(1 << 18, 1 << 16, 64, C.byref(n)) == 0
+    assert lib.cmt_quant_weight_bytes((1 << 18) + 1, 1 << 16, 64, C.byref(n)) == E and "2^34" in text(lib)
+    assert lib.cmt_quant_product(AT, 1, 64, 65535, AT, 1 << 21, 64, 32, None, 0, AT, 0, 1 << 21, None) == E and "2^36" in text(lib)
+    assert lib.cmt_beam_select_workspace(1 << 10, 32, 1 << 19, C.byref(n)) == 0
+    assert lib.cmt_beam_select_workspace(1 << 10, 32, (1 << 19) + 1, C.byref(n)) == E and "2^25" in text(lib)
+    job = (binding.CmtReorderTensor * 1)(binding.CmtReorderTensor(AT, 1 << 40, 8, 8, 8))
+    assert lib.cmt_beam_reorder(AT, (1 << 24) + 1, 4, job, 1, None) == E and "2^24" in text(lib)
+
+
+def test_a_target_on_the_rows_numbers_is_refused(lib):
+    job = lambda at: (binding.CmtReorderTensor * 1)(binding.CmtReorderTensor(AT, at, 8, 8, 8))
+    for at in (2 * AT, 2 * AT + 12, 2 * AT - 24):
+        assert lib.cmt_beam_reorder(2 * AT, 4, 4, job(at), 1, None) == E and "numbers" in text(lib), at

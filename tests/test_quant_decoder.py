@@ -187,3 +187,36 @@ def test_refusals():
         assert qd.beam_decode(src, n, 6, beam=4)[0].shape == (2, 6)
     finally:
         tr.close()
+
+
+@pytest.mark.parametrize("precision", [0, 1])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_many_rows_score_as_few(precision, group):
+    """1664 rows take another kernel for the layers' products than 128 do: a sentence scores the same."""
+    from paper_1802_07170_amd.decoding import QuantDecoder
+    c = I.CONFIGS["tiny"]
+    cfg = dict(I.model_cfg(c), hidden=512, layers=2)
+    src, n = I.make_batch(c)[:2]
+    tr = binding.Trainer(cfg, 1664, src.shape[1], 8, precision=precision)
+    try:
+        tr.init_params(3, 0.1)
+        qd = QuantDecoder(tr, group)
+        few = qd.beam_decode(src[:8], n[:8], 6, beam=16)[2]
+        many = qd.beam_decode(np.tile(src[:8], (13, 1)), np.tile(n[:8], 13), 6, beam=16)[2]
+        assert np.allclose(many, np.tile(few, 13), atol=LOOSE[precision])
+    finally:
+        tr.close()
+
+
+def test_lengths_of_another_batch_are_refused():
+    from paper_1802_07170_amd.decoding import QuantDecoder
+    cfg = dict(src_vocab=104, tgt_vocab=104, emb=16, hidden=32, layers=1)
+    tr = binding.Trainer(cfg, 8, 6, 6, precision=0)
+    try:
+        tr.init_params(1, 0.1)
+        qd = QuantDecoder(tr, 32)
+        for src, n in ((np.full((2, 6), 5), [6]), (np.full((2, 6), 5), [6, 6, 6]), (np.full(6, 5), [6])):
+            with pytest.raises(ValueError):
+                qd.beam_decode(np.array(src, np.int32), np.array(n, np.int32), 6, beam=2)
+    finally:
+        tr.close()
