@@ -48,7 +48,7 @@ def _pitch(t):
 def _call(f, device, *args):
     """f(*args, stream) with the tensors' device as the current one and its current stream.  (torch's own way to the
     stream's handle builds a Stream object for it: 1.9 us of the 4 that a launch takes.)"""
-    if device.index == torch.cuda.current_device():
+    if device.index == torch._C._cuda_getDevice():
         rc = f(*args, torch._C._cuda_getCurrentRawStream(device.index))
     else:
         with torch.cuda.device(device):
@@ -103,26 +103,29 @@ class QuantWeight:
 def quant_product(x, weight, bias=None, tanh=False, out_dtype=None, out=None):
     """x [rows, inputs] (fp32 or bf16) times the 4-bit weight's transpose, plus an fp32 bias [outputs], through tanh if asked for:
     [rows, outputs] in `out_dtype` (x's type if None), or in `out`."""
-    _tensor(x, "x", (2,), _TYPES, weight.device)
-    rows = x.shape[0]
-    if x.shape[1] != weight.inputs:
-        raise ValueError(f"x has {x.shape[1]} columns, the weight {weight.inputs} inputs")
+    packed, outputs, inputs = weight.packed, weight.outputs, weight.inputs
+    device = packed.device
+    _tensor(x, "x", (2,), _TYPES, device)
+    rows, columns = x.shape
+    if columns != inputs:
+        raise ValueError(f"x has {columns} columns, the weight {inputs} inputs")
     if bias is not None:
-        _tensor(bias, "bias", (1,), (torch.float32,), x.device)
-        if bias.shape[0] != weight.outputs:
-            raise ValueError(f"bias has {bias.shape[0]} elements, the weight {weight.outputs} outputs")
+        _tensor(bias, "bias", (1,), (torch.float32,), device)
+        if len(bias) != outputs:
+            raise ValueError(f"bias has {len(bias)} elements, the weight {outputs} outputs")
     if out is None:
         dtype = x.dtype if out_dtype is None else out_dtype
         if dtype not in _TYPES:
             raise ValueError(f"out_dtype must be torch.float32 or torch.bfloat16, not {dtype}")
-        out = torch.empty((rows, weight.outputs), dtype=dtype, device=x.device)
+        out, pitch = x.new_empty((rows, outputs), dtype=dtype), outputs
     else:
-        _tensor(out, "out", (2,), _TYPES if out_dtype is None else (out_dtype,), x.device)
-        if tuple(out.shape) != (rows, weight.outputs):
-            raise ValueError(f"out must be {(rows, weight.outputs)}, not {tuple(out.shape)}")
+        _tensor(out, "out", (2,), _TYPES if out_dtype is None else (out_dtype,), device)
+        if tuple(out.shape) != (rows, outputs):
+            raise ValueError(f"out must be {(rows, outputs)}, not {tuple(out.shape)}")
         _apart(out, "out", x, "x")
-    _call(binding.load_library().cmt_quant_product, x.device, x.data_ptr(), _TYPES[x.dtype], _pitch(x), rows, weight.packed.data_ptr(), weight.outputs,
-          weight.inputs, weight.group, None if bias is None else bias.data_ptr(), bool(tanh), out.data_ptr(), _TYPES[out.dtype], _pitch(out))
+        dtype, pitch = out.dtype, _pitch(out)
+    _call(binding.load_library().cmt_quant_product, device, x.data_ptr(), _TYPES[x.dtype], x.stride(0) if rows > 1 else inputs, rows, packed.data_ptr(),
+          outputs, inputs, weight.group, None if bias is None else bias.data_ptr(), bool(tanh), out.data_ptr(), _TYPES[dtype], pitch)
     return out
 
 
@@ -183,20 +186,22 @@ class SourceCache:
         r // (rows / sequences); query heads a multiple of the heads, in order.  Returns the same shape and type (0 for a sequence of
         length 0)."""
         self._filled()
-        _tensor(query, "query", (3,), _TYPES, self.device)
+        data = self.data
+        device = data.device
+        _tensor(query, "query", (3,), _TYPES, device)
         rows, heads, dim = query.shape
         if rows == 0 or rows % self.sequences or heads == 0 or heads % self.heads or dim != self.head_dim:
             raise ValueError(f"query must be (a multiple of {self.sequences}, a multiple of {self.heads}, {self.head_dim}), not {tuple(query.shape)}")
         if out is None:
-            out = torch.empty((rows, heads, dim), dtype=query.dtype, device=self.device)
+            out = query.new_empty((rows, heads, dim))
         else:
-            _tensor(out, "out", (3,), (query.dtype,), self.device)
+            _tensor(out, "out", (3,), (query.dtype,), device)
             if out.shape != query.shape:
                 raise ValueError(f"out must be {tuple(query.shape)}, not {tuple(out.shape)}")
             _apart(out, "out", query, "query")
-        for t, name in ((query, "query"), (out, "out")):
-            if heads > 1 and t.stride(1) != dim:
-                raise ValueError(f"{name}: the heads of a row must lie side by side")
+        q_pitch, o_pitch = query.stride(), out.stride()
+        if heads > 1 and (q_pitch[1] != dim or o_pitch[1] != dim):
+            raise ValueError(f"{'query' if q_pitch[1] != dim else 'out'}: the heads of a row must lie side by side")
         lib, per = binding.load_library(), rows // self.sequences
         key = (self.tokens, per, heads)
         need = self._needs.get(key)
@@ -204,9 +209,9 @@ class SourceCache:
             size = C.c_size_t()
             _check(lib.cmt_cache_attend_workspace(C.byref(self.config), per, heads, self.tokens, C.byref(size)))
             need = self._needs[key] = size.value
-        work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-        _call(lib.cmt_cache_attend, self.device, self.config, self.data.data_ptr(), query.data_ptr(), _TYPES[query.dtype],
-              query.stride(0) if rows > 1 else heads * dim, per, heads, self.tokens, scale, out.data_ptr(), out.stride(0) if rows > 1 else heads * dim,
+        work = data.new_empty(need) if need else None
+        _call(lib.cmt_cache_attend, device, self.config, data.data_ptr(), query.data_ptr(), _TYPES[query.dtype],
+              q_pitch[0] if rows > 1 else heads * dim, per, heads, self.tokens, scale, out.data_ptr(), o_pitch[0] if rows > 1 else heads * dim,
               None if work is None else work.data_ptr(), need)
         return out
 
@@ -229,19 +234,19 @@ def beam_select(logits, scores, n=None):
     there are fewer."""
     _tensor(logits, "logits", (2,), _TYPES)
     _tensor(scores, "scores", (2,), (torch.float32,), logits.device)
-    sentences, beam = scores.shape
-    if logits.shape[0] != sentences * beam:
-        raise ValueError(f"logits have {logits.shape[0]} rows, scores {sentences} x {beam} places")
+    (sentences, beam), (rows, vocab) = scores.shape, logits.shape
+    if rows != sentences * beam:
+        raise ValueError(f"logits have {rows} rows, scores {sentences} x {beam} places")
     if not scores.is_contiguous():
         raise ValueError("scores must be contiguous")
-    n, vocab, device = beam if n is None else n, logits.shape[1], logits.device
+    n, device, pitch = beam if n is None else n, logits.device, logits.stride(0) if rows > 1 else vocab
     need = _select_workspace(sentences, beam, vocab)
     if not isinstance(n, int) or n < 1:
         raise ValueError(f"n must be a positive number, not {n!r}")
-    new = torch.empty((sentences, n), dtype=torch.float32, device=device)
-    rows, tokens = torch.empty((2, sentences, n), dtype=torch.int32, device=device).unbind(0)
-    work = torch.empty(need, dtype=torch.uint8, device=device)
-    _call(binding.load_library().cmt_beam_select, device, logits.data_ptr(), _TYPES[logits.dtype], _pitch(logits), scores.data_ptr(), sentences, beam,
+    new = scores.new_empty((sentences, n))
+    rows, tokens = scores.new_empty((2, sentences, n), dtype=torch.int32).unbind(0)
+    work = scores.new_empty(need // 4)
+    _call(binding.load_library().cmt_beam_select, device, logits.data_ptr(), _TYPES[logits.dtype], pitch, scores.data_ptr(), sentences, beam,
           vocab, n, new.data_ptr(), rows.data_ptr(), tokens.data_ptr(), work.data_ptr(), need)
     return new, rows, tokens
 
