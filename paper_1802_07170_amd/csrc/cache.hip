@@ -12,17 +12,11 @@
 
 namespace cmt {
 
-// Nearest whole number to x / s, the even one of two, as if the quotient were exact.
-__device__ __forceinline__ int cache_code(float x, float s) {
-  if (s < 1e-36f) return (int)fmin(fmax(rint((double)x / (double)s), -127.0), 127.0);   // (1 / s may be infinite, s a rounded subnormal number)
-  float q = rintf(x / s);
-  const float r = fmaf(-q, s, x), r2 = 2.f * fabsf(r);       // (exact: |r| < 2 s and a multiple of half an ulp of s)
-  if (r2 > s || (r2 == s && ((int)q & 1))) q += copysignf(1.f, r);
-  return (int)q;
-}
-// The same of 16 numbers, packed: x inv + 1.5 2^23 has the code in its lowest bits, and is right wherever the remainder stays below half
-// a step; a slot with one that does not (a tie, or inv's rounding next to one) is made number by number.  (That for all: three times the instructions, which
-// bound the fill: 128 x 55 x 1024 31 us.)
+// The whole numbers nearest to 16 quotients x / s, the even one of two, as if the quotients were exact; packed.  x inv + 1.5 2^23 has the code in its
+// lowest bits, and is right wherever the remainder stays below half a step.  A slot with one that does not (a tie, or inv's rounding next to one) is
+// corrected by the remainders, which are exact (below 2 s and multiples of half an ulp of s); so is one of a scale so small that inv or a remainder
+// would leave fp32's range or precision, raised by a power of two (a scale rounded as a subnormal number: quotients up to 190).  (A division for
+// every number: three times the instructions, which bound the fill: 128 x 55 x 1024 31 us.)
 template <typename T>
 __device__ __forceinline__ void cache_codes(const Frag<T> (&x)[2], float s, float inv, uint32_t (&o)[4]) {
   const float big = 12582912.f;
@@ -34,9 +28,17 @@ __device__ __forceinline__ void cache_codes(const Frag<T> (&x)[2], float s, floa
     worst = fmaxf(worst, fabsf(fmaf(-(y - big), s, v)));
     c[e] = __float_as_uint(y);
   }
-  if (s < 1e-36f || !(2.f * worst < s))
+  if (s < 1e-36f || !(2.f * worst < s)) {
+    const float up = s < 1e-36f ? 0x1p64f : 1.f, step = s * up, per = 1.f / step;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) c[e] = (uint32_t)cache_code(x[e >> 3].get(e & 7), s);
+    for (int e = 0; e < 16; ++e) {
+      const float v = x[e >> 3].get(e & 7) * up;
+      float q = fmaf(v, per, big) - big;
+      const float r = fmaf(-q, step, v), r2 = 2.f * fabsf(r);
+      if (r2 > step || (r2 == step && ((int)q & 1))) q += copysignf(1.f, r);
+      c[e] = (uint32_t)(int)fminf(fmaxf(q, -127.f), 127.f);
+    }
+  }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const uint32_t lo = __builtin_amdgcn_perm(c[4 * k + 1], c[4 * k], 0x0c0c0400), hi = __builtin_amdgcn_perm(c[4 * k + 3], c[4 * k + 2], 0x04000c0c);
@@ -51,11 +53,12 @@ __device__ __forceinline__ void fill_load(const T* p, int n, bool wide, Frag<T> 
   else { load_elements(p, n, x[0]); load_elements(p + 8, n - 8, x[1]); }
 }
 // One workgroup per block of 32 tokens, sequence and head (of few d: as many blocks as have a wavefront for every 32 d); blockIdx.z:
-// keys, values.  A block is read once: a thread keeps its NS slots of 16 d of a token until the scale is known.  (16 d, 4 heads x 7604
-// tokens, a workgroup per block: 29 us.)
+// keys, values.  A block is read once: a thread keeps its NS slots of 16 d of a token until the scale is known; 16-bit rows
+// take the registers of three workgroups to a CU (96 d, 3 x 22432 tokens 22 -> 16 us).  Bound by the phases of a block, read, code, write, of which a
+// CU holds three at a time: 128 x 55 x 1024 in 16 bits, 43 MB, 20 us.  (16 d, 4 heads x 7604 tokens, a workgroup per block: 29 us.)
 __host__ __device__ inline int fill_blocks(int chunks) { return chunks > 4 ? 1 : 8 / chunks; }
 template <typename T, int NS>
-__global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const int32_t* __restrict__ lengths, int tokens, CacheShape s, CacheView c, int wide) {
+__global__ __launch_bounds__(512, sizeof(T) == 2 ? 6 : 4) void cache_fill_kernel(CacheSource src, const int32_t* __restrict__ lengths, int tokens, CacheShape s, CacheView c, int wide) {
   __shared__ uint4 code[512 * NS];                           // in the cache's order
   __shared__ uint32_t s_most[8];
   const int b = s.heads == 1 ? blockIdx.y : blockIdx.y / s.heads, head = blockIdx.y - b * s.heads, t = threadIdx.x, lane = t & 63;
@@ -63,22 +66,23 @@ __global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const 
   const bool is_v = blockIdx.z;
   const int len = min(max(lengths[b], 0), tokens);
   if (t == 0 && head == 0 && blockIdx.x == 0 && !is_v) c.lengths[b] = len;
-  const int chunks = s.chunks(), slots = chunks * 64;        // at most 512 NS: token i % 32, d = 16 (i / 32) + 0..15
+  const int chunks = s.chunks(), slots = chunks * 64;        // at most 512 NS
   const int together = fill_blocks(chunks), mine = together == 1 ? 0 : w / chunks, w0 = mine * chunks, wn = together == 1 ? 8 : chunks;   // the block's wavefronts
   const int blk = blockIdx.x * together + mine, i0 = together == 1 ? t : t - 64 * w0;
+  // Slot k 512 + i0: 16 d of a token, the thread's next one 256 d on.  Four lanes side by side are four tokens (their bytes are turned over below), the
+  // next bits d: a load takes 128 bytes of 16 tokens (where the chunks are odd 64 of 32).
+  const bool pairs = !(chunks & 1);
+  const int r = (i0 & 3) | (pairs ? i0 >> 2 & 28 : i0 >> 1 & 28), d16_0 = pairs ? (i0 >> 2 & 3) | i0 >> 7 << 2 : (i0 >> 2 & 1) | i0 >> 6 << 1;
   const int n = mine < together ? min(len - blk * CACHE_BLOCK, CACHE_BLOCK) : 0;   // valid tokens of the block (none: nothing reads it)
   if (blockIdx.x * together * CACHE_BLOCK >= len) return;
   const size_t tok = is_v ? src.v_tok : src.k_tok;
   const T* p = (const T*)(is_v ? src.v : src.k) + (size_t)b * (is_v ? src.v_seq : src.k_seq) + (size_t)head * (is_v ? src.v_head : src.k_head) +
-               (size_t)blk * CACHE_BLOCK * tok;
+               ((size_t)blk * CACHE_BLOCK + r) * tok + 16 * d16_0;
   const bool wd = wide >> is_v & 1;
   Frag<T> x[NS][2];                                          // as they come: 16-bit ones take half the registers
   uint32_t bits = 0;                                         // the largest without its sign: as numbers, infinities and NaN above all
 #pragma unroll
-  for (int k = 0; k < NS; ++k) {
-    const int i = k * 512 + i0, r = i & 31, d = 16 * (i >> 5);
-    fill_load(p + (size_t)r * tok + d, i < slots && r < n ? s.dim - d : 0, wd, x[k]);
-  }
+  for (int k = 0; k < NS; ++k) fill_load(p + 256 * k, k * 512 + i0 < slots && r < n ? s.dim - 16 * d16_0 - 256 * k : 0, wd, x[k]);
 #pragma unroll
   for (int k = 0; k < NS; ++k)
 #pragma unroll
@@ -99,7 +103,7 @@ __global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const 
   uint4* const block = code + 64 * w0;
 #pragma unroll
   for (int k = 0; k < NS; ++k) {
-    const int i = k * 512 + i0, r = i & 31, d16 = i >> 5;
+    const int i = k * 512 + i0, d16 = d16_0 + 16 * k;
     uint32_t o[4] = {0, 0, 0, 0};
     if (some) cache_codes(x[k], scale, inv, o);
     if (!is_v) {
@@ -121,9 +125,9 @@ __global__ __launch_bounds__(512) void cache_fill_kernel(CacheSource src, const 
                            (uint32_t)__builtin_amdgcn_update_dpp(0, give(3), 0x1b, 0xf, 0xf, true)};
     uint32_t a[4];                                           // by token: g[j] came from lane ^ j
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int j = (lane ^ r) & 3;
-      a[r] = j == 0 ? g[0] : j == 1 ? g[1] : j == 2 ? g[2] : g[3];
+    for (int u = 0; u < 4; ++u) {
+      const int j = (lane ^ u) & 3;
+      a[u] = j == 0 ? g[0] : j == 1 ? g[1] : j == 2 ? g[2] : g[3];
     }
     const uint32_t p01 = __builtin_amdgcn_perm(a[1], a[0], 0x05010400), q01 = __builtin_amdgcn_perm(a[1], a[0], 0x07030602);   // d 0 1 and 2 3 of tokens 0, 1
     const uint32_t p23 = __builtin_amdgcn_perm(a[3], a[2], 0x05010400), q23 = __builtin_amdgcn_perm(a[3], a[2], 0x07030602);

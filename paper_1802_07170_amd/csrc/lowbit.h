@@ -154,13 +154,5 @@ __device__ __forceinline__ void operand_of(const Frag<float>& x, bool in, Frag<b
   f[1].v = make_uint4(m[0], m[1], m[2], m[3]);
   f[2].v = make_uint4(l[0], l[1], l[2], l[3]);
 }
-// the first n of 8 elements as operand parts; wide: p is a multiple of 16 bytes
-template <typename T>
-__device__ __forceinline__ void load_operand(const T* p, int n, bool wide, Frag<bf16_t> (&f)[OPERAND_PARTS<T>]) {
-  Frag<T> x;
-  if (n >= 8 && wide) x.load(p);
-  else load_elements(p, n, x);
-  operand_of(x, true, f);
-}
 
 }  // namespace cmt
