@@ -443,3 +443,48 @@ def test_refusals_on_the_device(D):
     for bad in (x[:2, None], x[:, None, :32], x[:, None].half()):
         with pytest.raises(ValueError):
             cache.attend(bad)
+
+
+# ---- offsets that 32 bits do not hold: exact cases whose answer lies behind the 2^32nd byte ------------------------
+def test_a_weight_of_more_than_4_gib_of_codes(D):
+    n, k = (1 << 17) + 16, 1 << 16
+    w = torch.zeros(n, k, dtype=BF, device="cuda")
+    w[-1] = torch.tensor([6.0, -4.0, 0.5, 3.0], device="cuda").repeat(k // 4)       # the scale is 1: the codes are exact
+    weight = D.QuantWeight.pack(w, 128)
+    assert weight.packed.numel() > 1 << 32
+    del w
+    x = (torch.arange(2 * k, device="cuda").view(2, k) % 3).to(BF)                # sums below 2^24
+    want = (x.double() * torch.tensor([6.0, -4.0, 0.5, 3.0], device="cuda").repeat(k // 4).double()).sum(1)
+    y = D.quant_product(x, weight, out_dtype=FP)
+    assert torch.equal(y[:, -1].double(), want) and not y[:, :-1].any()
+
+
+def test_a_cache_of_more_than_4_gib(D):
+    tokens = (1 << 22) + 40
+    x = torch.zeros(1, tokens, 1, 1024, dtype=BF, device="cuda")
+    row = (torch.arange(1024, device="cuda") % 255 - 127).to(BF)                  # the scale is 1: the codes are exact
+    x[0, tokens - 3, 0] = row
+    cache = D.SourceCache(1, 1, 1024, tokens).fill(x, x, torch.tensor([tokens], dtype=torch.int32, device="cuda"))
+    assert cache.data.numel() > 1 << 33
+    q = torch.sign(row)[None, None].contiguous()                                  # its score is far above the others', which are 0
+    assert torch.equal(cache.attend(q)[0, 0], row)
+    assert not cache.attend(-q).isnan().any()
+
+
+def test_logits_of_more_than_2_to_the_32(D):
+    sentences, beam, vocab = 4112, 2, 1 << 19
+    logits = torch.empty(sentences * beam, vocab, dtype=BF, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(7))
+    scores = -torch.rand(sentences, beam, generator=torch.Generator(device="cuda").manual_seed(8), device="cuda")
+    assert logits.numel() > 1 << 32
+    new, rows, tokens = D.beam_select(logits, scores)
+    last = 3
+    few = D.beam_select(logits[-last * beam:], scores[-last:])
+    assert torch.equal(new[-last:], few[0]) and torch.equal(rows[-last:], few[1] + (sentences - last) * beam) and torch.equal(tokens[-last:], few[2])
+
+
+def test_rows_of_a_gib(D):
+    source = torch.zeros(5, 1 << 30, dtype=torch.uint8, device="cuda")
+    source[:, -1] = torch.arange(1, 6, device="cuda")
+    target = torch.full((6, 1 << 30), 9, dtype=torch.uint8, device="cuda")
+    D.beam_reorder(torch.tensor([4, 0, -1, 5, 4, 3], dtype=torch.int32, device="cuda"), [source], [target])
+    assert target[:, -1].tolist() == [5, 1, 9, 9, 5, 4] and target[:, 0].tolist() == [0, 0, 9, 9, 0, 0]
