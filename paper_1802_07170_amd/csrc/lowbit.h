@@ -125,8 +125,9 @@ __device__ __forceinline__ uint32_t pack_hi(uint32_t lo, uint32_t hi) { return _
 
 // Operand parts of 8 consecutive elements: 1 of bf16, 3 of fp32.
 template <typename T> constexpr int OPERAND_PARTS = sizeof(T) == 2 ? 1 : 3;
-// the first n (or all 8) elements at p, 0 behind them
+// the first n (or all 8) elements at p, wherever p is, 0 behind them
 __device__ __forceinline__ void load_elements(const bf16_t* p, int n, Frag<bf16_t>& f) {
+  if (n >= 8) { __builtin_memcpy(&f.v, p, 16); return; }
   uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -134,11 +135,35 @@ __device__ __forceinline__ void load_elements(const bf16_t* p, int n, Frag<bf16_
   f.v = make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ void load_elements(const float* p, int n, Frag<float>& f) {
+  if (n >= 8) { __builtin_memcpy(&f.lo, p, 16); __builtin_memcpy(&f.hi, p + 4, 16); return; }
   float x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : 0.f;
   f.lo = make_float4(x[0], x[1], x[2], x[3]);
   f.hi = make_float4(x[4], x[5], x[6], x[7]);
+}
+// The same in two steps, so that many loads go out one behind the other, of a row of 8 elements or more: those from `at` on, near the row's end its last 8,
+// and their move to where they belong, 0 behind them.
+template <typename T>
+__device__ __forceinline__ void load_near(const T* row, int at, int size, Frag<T>& f) { load_elements(row + min(at, size - 8), 8, f); }
+__device__ __forceinline__ void move_near(int at, int size, Frag<bf16_t>& f) {
+  const int by = at - (size - 8);
+  if (by <= 0) return;
+  uint4 v = f.v;
+  if (by & 1) v = make_uint4(v.x >> 16 | v.y << 16, v.y >> 16 | v.z << 16, v.z >> 16 | v.w << 16, v.w >> 16);
+  if (by & 2) v = make_uint4(v.y, v.z, v.w, 0);
+  if (by & 4) v = make_uint4(v.z, v.w, 0, 0);
+  f.v = by < 8 ? v : make_uint4(0, 0, 0, 0);
+}
+__device__ __forceinline__ void move_near(int at, int size, Frag<float>& f) {
+  const int by = at - (size - 8);
+  if (by <= 0) return;
+  float4 a = f.lo, b = f.hi;
+  if (by & 1) { a = make_float4(a.y, a.z, a.w, b.x); b = make_float4(b.y, b.z, b.w, 0.f); }
+  if (by & 2) { a = make_float4(a.z, a.w, b.x, b.y); b = make_float4(b.z, b.w, 0.f, 0.f); }
+  if (by & 4) { a = b; b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  f.lo = by < 8 ? a : make_float4(0.f, 0.f, 0.f, 0.f);
+  f.hi = by < 8 ? b : make_float4(0.f, 0.f, 0.f, 0.f);
 }
 __device__ __forceinline__ void operand_of(const Frag<bf16_t>& x, bool in, Frag<bf16_t> (&f)[1]) {   // in = false: zeros
   f[0].v = make_uint4(in ? x.v.x : 0u, in ? x.v.y : 0u, in ? x.v.z : 0u, in ? x.v.w : 0u);

@@ -175,18 +175,25 @@ __global__ __launch_bounds__(64 * QUANT_WAVES) void quant_product_kernel(const T
       for (int g = 0; g < PER; ++g) sc[i][g] = *reinterpret_cast<const uint2*>(scales + (tile * PER + g) * 16 + 4 * q);
     }
     Frag<bf16_t> xf[CT][4][PARTS];
+    Frag<T> xr[CT][4];
+    auto each = [&](auto f) {                                // f(row of x, k, the fragment)
 #pragma unroll
-    for (int j = 0; j < CT; ++j) {
-      const int m = m0 + 16 * j + c;
+      for (int j = 0; j < CT; ++j)
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int k = kt * QUANT_TILE_K + 32 * s + 8 * q;
-        Frag<T> f;
-        if constexpr (WHOLE) f.load(x + (size_t)min(m, M - 1) * ldx + (k < K ? k : 0));   // (rows beyond M: not stored)
-        else load_elements(x + (m < M ? (size_t)m * ldx + k : 0), m < M ? K - k : 0, f);
-        operand_of(f, !WHOLE || k < K, xf[j][s]);
-      }
+        for (int s = 0; s < 4; ++s) f(x + (size_t)min(m0 + 16 * j + c, M - 1) * ldx, kt * QUANT_TILE_K + 32 * s + 8 * q, xr[j][s]);   // (rows beyond M: not stored)
+    };
+    if constexpr (WHOLE) {
+      each([&](const T* row, int k, Frag<T>& f) { f.load(row + (k < K ? k : 0)); });
+    } else if (K >= 8) {
+      each([&](const T* row, int k, Frag<T>& f) { load_near(row, k, K, f); });
+      if (kt == k_tiles - 1) each([&](const T*, int k, Frag<T>& f) { move_near(k, K, f); });
+    } else {
+      each([&](const T* row, int k, Frag<T>& f) { load_elements(row + k, K - k, f); });
     }
+#pragma unroll
+    for (int j = 0; j < CT; ++j)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) operand_of(xr[j][s], !WHOLE || kt * QUANT_TILE_K + 32 * s + 8 * q < K, xf[j][s]);
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -306,12 +313,16 @@ __global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T*
         sn[i][g] = *reinterpret_cast<const uint2*>(sp + (((size_t)min(nb + i, row_blocks - 1) * k_tiles + kt) * PER + g) * 16);
     }
     if constexpr (DIRECT) return;
+    auto each = [&](auto f) {                                // f(row of x, k, the fragment)
 #pragma unroll
-    for (int u = 0; u < MINE; ++u) {
-      const int slot = u * THREADS + threadIdx.x, m = m0 + (slot >> 4), k = kt * QUANT_TILE_K + 8 * chunk_of(slot);
-      if constexpr (WHOLE) xn[u].load(x + (size_t)min(m, M - 1) * ldx + (k < K ? k : 0));   // (rows beyond M: not stored)
-      else load_elements(x + (m < M ? (size_t)m * ldx + k : 0), m < M ? K - k : 0, xn[u]);
-    }
+      for (int u = 0; u < MINE; ++u) {
+        const int slot = u * THREADS + threadIdx.x;
+        f(x + (size_t)min(m0 + (slot >> 4), M - 1) * ldx, kt * QUANT_TILE_K + 8 * chunk_of(slot), xn[u]);   // (rows beyond M: not stored)
+      }
+    };
+    if constexpr (WHOLE) each([&](const T* row, int k, Frag<T>& f) { f.load(row + (k < K ? k : 0)); });
+    else if (K >= 8) each([&](const T* row, int k, Frag<T>& f) { load_near(row, k, K, f); });
+    else each([&](const T* row, int k, Frag<T>& f) { load_elements(row + k, K - k, f); });
   };
   if constexpr (DIRECT) request(0, xs[0][0]);
   fetch(0);
@@ -322,6 +333,8 @@ __global__ __launch_bounds__(QUANT_WIDE) void quant_product_wide_kernel(const T*
     for (int u = 0; u < MINE; ++u) {
       const int slot = u * THREADS + threadIdx.x;
       Frag<bf16_t> f[PARTS];
+      if constexpr (!WHOLE)
+        if (kt == k_tiles - 1 && K >= 8) move_near(kt * QUANT_TILE_K + 8 * chunk_of(slot), K, xn[u]);
       operand_of(xn[u], !WHOLE || kt * QUANT_TILE_K + 8 * chunk_of(slot) < K, f);
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) buf[p][slot] = f[p].v;
