@@ -48,8 +48,8 @@ __device__ __forceinline__ void cache_codes(const Frag<T> (&x)[2], float s, floa
 
 // ---- writing ---------------------------------------------------------------------------------------------
 template <typename T>
-__device__ __forceinline__ void fill_load(const T* p, int n, bool wide, Frag<T> (&x)[2]) {   // the first n of 16 elements, then 0
-  if (n >= 16 && wide) { x[0].load(p); x[1].load(p + 8); }
+__device__ __forceinline__ void fill_load(const T* p, int n, Frag<T> (&x)[2]) {   // the first n of 16 elements, then 0
+  if (n >= 16) { load_elements(p, 8, x[0]); load_elements(p + 8, 8, x[1]); }
   else { load_elements(p, n, x[0]); load_elements(p + 8, n - 8, x[1]); }
 }
 // One workgroup per block of 32 tokens, sequence and head (of few d: as many blocks as have a wavefront for every 32 d); blockIdx.z:
@@ -58,7 +58,7 @@ __device__ __forceinline__ void fill_load(const T* p, int n, bool wide, Frag<T> 
 // CU holds three at a time: 128 x 55 x 1024 in 16 bits, 43 MB, 20 us.  (16 d, 4 heads x 7604 tokens, a workgroup per block: 29 us.)
 __host__ __device__ inline int fill_blocks(int chunks) { return chunks > 4 ? 1 : 8 / chunks; }
 template <typename T, int NS>
-__global__ __launch_bounds__(512, sizeof(T) == 2 ? 6 : 4) void cache_fill_kernel(CacheSource src, const int32_t* __restrict__ lengths, int tokens, CacheShape s, CacheView c, int wide) {
+__global__ __launch_bounds__(512, sizeof(T) == 2 ? 6 : 4) void cache_fill_kernel(CacheSource src, const int32_t* __restrict__ lengths, int tokens, CacheShape s, CacheView c) {
   __shared__ uint4 code[512 * NS];                           // in the cache's order
   __shared__ uint32_t s_most[8];
   const int b = s.heads == 1 ? blockIdx.y : blockIdx.y / s.heads, head = blockIdx.y - b * s.heads, t = threadIdx.x, lane = t & 63;
@@ -78,11 +78,10 @@ __global__ __launch_bounds__(512, sizeof(T) == 2 ? 6 : 4) void cache_fill_kernel
   const size_t tok = is_v ? src.v_tok : src.k_tok;
   const T* p = (const T*)(is_v ? src.v : src.k) + (size_t)b * (is_v ? src.v_seq : src.k_seq) + (size_t)head * (is_v ? src.v_head : src.k_head) +
                ((size_t)blk * CACHE_BLOCK + r) * tok + 16 * d16_0;
-  const bool wd = wide >> is_v & 1;
   Frag<T> x[NS][2];                                          // as they come: 16-bit ones take half the registers
   uint32_t bits = 0;                                         // the largest without its sign: as numbers, infinities and NaN above all
 #pragma unroll
-  for (int k = 0; k < NS; ++k) fill_load(p + 256 * k, k * 512 + i0 < slots && r < n ? s.dim - 16 * d16_0 - 256 * k : 0, wd, x[k]);
+  for (int k = 0; k < NS; ++k) fill_load(p + 256 * k, k * 512 + i0 < slots && r < n ? s.dim - 16 * d16_0 - 256 * k : 0, x[k]);
 #pragma unroll
   for (int k = 0; k < NS; ++k)
 #pragma unroll
@@ -144,13 +143,10 @@ __global__ __launch_bounds__(512, sizeof(T) == 2 ? 6 : 4) void cache_fill_kernel
     for (int i = i0; i < slots; i += 512) reinterpret_cast<uint4*>(out)[i] = block[i];
 }
 void launch_cache_fill(int prec, const CacheSource& src, const int32_t* lengths, int tokens, const CacheShape& s, void* cache, hipStream_t st) {
-  const size_t es = prec ? 2 : 4;
-  auto wide = [&](const void* p, size_t a, size_t b, size_t c) { return (((uintptr_t)p | a * es | b * es | c * es) & 15) == 0; };
-  const int flags = (wide(src.k, src.k_seq, src.k_tok, src.k_head) ? 1 : 0) | (wide(src.v, src.v_seq, src.v_tok, src.v_head) ? 2 : 0);
   const int blocks = (tokens + CACHE_BLOCK - 1) / CACHE_BLOCK, together = fill_blocks(s.chunks());
   const dim3 grid((unsigned)((blocks + together - 1) / together), (unsigned)(s.seqs * s.heads), 2);
   auto go = [&](auto type, auto ns) {
-    hipLaunchKernelGGL((cache_fill_kernel<decltype(type), decltype(ns)::value>), grid, dim3(512), 0, st, src, lengths, tokens, s, CacheView(s, cache), flags);
+    hipLaunchKernelGGL((cache_fill_kernel<decltype(type), decltype(ns)::value>), grid, dim3(512), 0, st, src, lengths, tokens, s, CacheView(s, cache));
   };
   auto by_width = [&](auto type) {
     if (s.chunks() <= 8) go(type, std::integral_constant<int, 1>());
@@ -163,7 +159,7 @@ void launch_cache_fill(int prec, const CacheSource& src, const int32_t* lengths,
 // ---- reading back: [seqs, tokens, heads, dim], 0 behind a sequence's end -------------------------------------
 // One workgroup per block, sequence and head; blockIdx.z: keys, values.  The block's codes pass through LDS as they are.
 // Bound by the fp32 rows that it writes (128 x 80 x 1024 twice, 84 MB: 19.6 us).
-__global__ __launch_bounds__(256) void cache_read_kernel(CacheShape s, CacheView c, int tokens, int wide, float* __restrict__ k, float* __restrict__ v) {
+__global__ __launch_bounds__(256) void cache_read_kernel(CacheShape s, CacheView c, int tokens, float* __restrict__ k, float* __restrict__ v) {
   __shared__ uint4 code[2048];
   const int b = blockIdx.y / s.heads, head = blockIdx.y % s.heads, blk = blockIdx.x, t = threadIdx.x;
   const bool is_v = blockIdx.z;
@@ -191,15 +187,14 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheShape s, CacheView
       for (int e = 0; e < 4; ++e) x[e] = (float)o[((cell + (is_v ? e : 0) + row) & 15) * 16 + (is_v ? 0 : e)] * scale;
     }
     float* const to = out + r * row + d;
-    if (wide) *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+    if (s.dim % 4 == 0 || d + 4 <= s.dim) store_four(to, x[0], x[1], x[2], x[3]);
     else
       for (int e = 0; e < 4; ++e) if (d + e < s.dim) to[e] = x[e];
   }
 }
 void launch_cache_read(const CacheShape& s, const void* cache, int tokens, float* k, float* v, hipStream_t st) {
   const dim3 grid((unsigned)((tokens + CACHE_BLOCK - 1) / CACHE_BLOCK), (unsigned)(s.seqs * s.heads), 2);
-  const int wide = s.dim % 4 == 0 && (((uintptr_t)k | (uintptr_t)v) & 15) == 0;
-  hipLaunchKernelGGL(cache_read_kernel, grid, dim3(256), 0, st, s, CacheView(s, const_cast<void*>(cache)), tokens, wide, k, v);
+  hipLaunchKernelGGL(cache_read_kernel, grid, dim3(256), 0, st, s, CacheView(s, const_cast<void*>(cache)), tokens, k, v);
 }
 
 // ---- the attention -------------------------------------------------------------------------------------------
@@ -236,7 +231,7 @@ size_t cache_attend_workspace(const CacheShape& s, int per, int q_heads, int tok
 
 struct AttendArgs {
   const void* q; size_t ldq; void* out; size_t ldo;
-  int per, share, splits, tokens, wide_q, wide_o;           // queries in aligned pieces of 8; results of 4
+  int per, share, splits, tokens;
   float scale;
   float* ml; float* part;                                    // of ranges: (maximum, sum) [unit][range][tile], products [unit][range][tile][32 chunks]
 };
@@ -307,7 +302,7 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
 #pragma unroll
       for (int u = 0; u < EPW; ++u) {
         const int d = 32 * (u * 8 + w) + 8 * q4;
-        if (a.wide_q) raw[x][u].load(qp + (d < s.dim ? d : 0));
+        if (s.dim >= 8) load_near(qp, d, s.dim, raw[x][u]);
         else load_elements(qp + d, in ? s.dim - d : 0, raw[x][u]);
       }
     }
@@ -316,6 +311,7 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
 #pragma unroll
       for (int u = 0; u < EPW; ++u) {
         Frag<bf16_t> f[QP];
+        if (s.dim >= 8 && s.dim % 8) move_near(32 * (u * 8 + w) + 8 * q4, s.dim, raw[x][u]);
         operand_of(raw[x][u], 32 * (u * 8 + w) + 8 * q4 < s.dim && g0 + 16 * x + g < G, f);
         if (u * 8 + w < E)
 #pragma unroll
@@ -483,7 +479,6 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
     }
     return;
   }
-  struct alignas(4 * sizeof(T)) Four { T v[4]; };
 #pragma unroll
   for (int x = 0; x < GT; ++x) {
     if (g0 + 16 * x + g >= G) continue;
@@ -498,11 +493,12 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
         for (int h = 0; h < 2; ++h) {
           const int d = 32 * (mine + e) + 16 * h + 4 * q4;
           const v4f& y = acc[x][e][h];
-          const Four o{{from_f<T>(y[0] * inv), from_f<T>(y[1] * inv), from_f<T>(y[2] * inv), from_f<T>(y[3] * inv)}};
-          if (a.wide_o) { if (d < s.dim) *reinterpret_cast<Four*>(out + d) = o; }
+          if (s.dim % 4 == 0) {
+            if (d < s.dim) store_four(out + d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+          } else if (d + 4 <= s.dim) store_four(out + d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
           else
 #pragma unroll
-            for (int i = 0; i < 4; ++i) if (d + i < s.dim) out[d + i] = o.v[i];
+            for (int i = 0; i < 4; ++i) if (d + i < s.dim) out[d + i] = from_f<T>(y[i] * inv);
         }
   }
 }
@@ -556,13 +552,10 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a, CacheShap
 void launch_cache_attend(int prec, const CacheShape& s, const void* cache, const void* q, size_t ldq, int per, int q_heads, int tokens, float scale,
                          void* out, size_t ldo, void* workspace, hipStream_t st) {
   const AttendPlan p = attend_plan(s, per, q_heads, tokens);
-  const size_t es = prec ? 2 : 4;
   const long units = (long)s.seqs * s.heads * p.g_tiles;
   AttendArgs a{};
   a.q = q; a.ldq = ldq; a.out = out; a.ldo = ldo; a.per = per; a.share = q_heads / s.heads; a.splits = p.splits;
   a.tokens = tokens; a.scale = scale;
-  a.wide_q = (((uintptr_t)q | ldq * es) & 15) == 0 && s.dim % 8 == 0;
-  a.wide_o = (((uintptr_t)out | ldo * es | s.dim * es) & (4 * es - 1)) == 0;
   a.ml = (float*)workspace; a.part = a.ml + (size_t)units * p.splits * p.tile * 2;
   auto go = [&](auto type, auto epw, auto gt, auto blk) {
     using T = decltype(type);

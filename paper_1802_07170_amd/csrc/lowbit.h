@@ -125,6 +125,11 @@ __device__ __forceinline__ uint32_t pack_hi(uint32_t lo, uint32_t hi) { return _
 
 // Operand parts of 8 consecutive elements: 1 of bf16, 3 of fp32.
 template <typename T> constexpr int OPERAND_PARTS = sizeof(T) == 2 ? 1 : 3;
+// four elements that lie anywhere, stored as one
+typedef float any_v4f __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t any_v4h __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void store_four(float* p, float a, float b, float c, float d) { *reinterpret_cast<any_v4f*>(p) = any_v4f{a, b, c, d}; }
+__device__ __forceinline__ void store_four(bf16_t* p, float a, float b, float c, float d) { *reinterpret_cast<any_v4h*>(p) = any_v4h{f2bf(a), f2bf(b), f2bf(c), f2bf(d)}; }
 // the first n (or all 8) elements at p, wherever p is, 0 behind them
 __device__ __forceinline__ void load_elements(const bf16_t* p, int n, Frag<bf16_t>& f) {
   if (n >= 8) { __builtin_memcpy(&f.v, p, 16); return; }

@@ -104,7 +104,7 @@ void launch_quant_values(const void* packed, const QuantShape& q, float* out, hi
                      (const bf16_t*)((const char*)packed + q.code_bytes()), q, q.k_tiles(), out);
 }
 
-// Four neighbouring outputs of row m; flags: 1 tanh, 2 y in bf16, 8 y takes them in one piece, 16 they are the gates of an LSTM's unit.
+// Four neighbouring outputs of row m; flags: 1 tanh, 2 y in bf16, 16 they are the gates of an LSTM's unit.
 // An LSTM layer's weight is packed with a unit's four gates side by side, so that the lane that ends up with them makes the unit's cell: no
 // gates in memory and no launch for the cells (10 rows, width 1024: 5.0 us a layer against 4.4 + 2.6; 640 rows 38 against 37 + 5).
 struct QuantCell { const float* c_prev; float* c; void *h, *h2; size_t ldh, ldh2; };
@@ -130,12 +130,12 @@ __device__ __forceinline__ void quant_store(float a, float b, float c, float d, 
   }
   if (flags & 2) {
     bf16_t* o = (bf16_t*)y + (size_t)m * ldy + n;
-    if ((flags & 8) && n + 4 <= N) *reinterpret_cast<uint2*>(o) = make_uint2(f2bf(r[0]) | (uint32_t)f2bf(r[1]) << 16, f2bf(r[2]) | (uint32_t)f2bf(r[3]) << 16);
+    if (n + 4 <= N) store_four(o, r[0], r[1], r[2], r[3]);
     else
       for (int e = 0; e < 4; ++e) if (n + e < N) o[e] = f2bf(r[e]);
   } else {
     float* o = (float*)y + (size_t)m * ldy + n;
-    if ((flags & 8) && n + 4 <= N) *reinterpret_cast<float4*>(o) = make_float4(r[0], r[1], r[2], r[3]);
+    if (n + 4 <= N) store_four(o, r[0], r[1], r[2], r[3]);
     else
       for (int e = 0; e < 4; ++e) if (n + e < N) o[e] = r[e];
   }
@@ -431,7 +431,9 @@ static void quant_product_wide_go(const void* x, size_t ldx, const QuantWeightRe
 //   scales of its groups: 160 rows with groups of 128, 128 of 64) where rounds of workgroups times their rows are fewer: 640 rows 62 against 78, 128 rows 28 against 18.
 //   Else two tiles of rows to a workgroup where there are two (640 rows 108 against 129; fp32, whose parts are three times the registers, 285
 //   against 226: one), and four row blocks of the weight, which share x, where one each would be 512 workgroups or more (4096 x 2048, 128 rows
-//   11 against 18; 512 x 4096 in fp32, 128 rows 17 against 12).
+//   11 against 18; 512 x 4096 in fp32, 128 rows 17 against 12).  Few rows of many inputs have little to share (without the host's share: 10000 x 4096, 1 | 4 | 8
+//   rows 13 against 8.3 | 9.6 | 11.6; 16000 x 2048, 1 | 4 | 8 rows 8.4 against 6.6 | 7.4 | 8.7; 30000 x 1024, 1 | 2 | 4 rows 6.9 against 6.6 | 6.6 | 7.5): one
+//   row block from 512 inputs a row on (in fp32 the parts cost more than that: 16.7 against 20.7).
 template <typename T, int GROUP>
 static void quant_product_tiles(const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, int flags, void* y, size_t ldy,
                                 const QuantCell& cell, hipStream_t st) {
@@ -450,7 +452,7 @@ static void quant_product_tiles(const void* x, size_t ldx, const QuantWeightRef&
       else quant_product_go<T, GROUP, 4, CT>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
       return;
     }
-  if (rb * ((M + 15) / 16) < 512) quant_product_go<T, GROUP, 1, 1>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
+  if (rb * ((M + 15) / 16) < 512 || (sizeof(T) == 2 && 512l * M <= w.shape.K)) quant_product_go<T, GROUP, 1, 1>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
   else quant_product_go<T, GROUP, 4, 1>(x, ldx, w, M, bias, flags, y, ldy, cell, st);
 }
 static void quant_product_any(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, int flags, void* y, size_t ldy,
@@ -466,9 +468,7 @@ static void quant_product_any(int prec, const void* x, size_t ldx, const QuantWe
 }
 void launch_quant_product(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, bool tanh, int y_prec, void* y,
                           size_t ldy, hipStream_t st) {
-  const size_t ys = y_prec ? 2 : 4;
-  const int flags = (tanh ? 1 : 0) | (y_prec ? 2 : 0) | (((uintptr_t)y | ldy * ys) % (4 * ys) == 0 ? 8 : 0);
-  quant_product_any(prec, x, ldx, w, M, bias, flags, y, ldy, QuantCell{}, st);
+  quant_product_any(prec, x, ldx, w, M, bias, (tanh ? 1 : 0) | (y_prec ? 2 : 0), y, ldy, QuantCell{}, st);
 }
 void launch_quant_lstm(int prec, const void* x, size_t ldx, const QuantWeightRef& w, int M, const float* bias, const float* c_prev, float* c, void* h,
                        size_t ldh, void* h2, size_t ldh2, hipStream_t st) {

@@ -18,7 +18,7 @@ __device__ __forceinline__ unsigned search_sortable(float v) {   // larger numbe
 // ---- statistics of the groups ---------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void search_groups_kernel(const T* __restrict__ logits, size_t ld, const float* __restrict__ scores, int rows, int V,
-                                                            int groups, int wide, float2* __restrict__ stat) {
+                                                            int groups, float2* __restrict__ stat) {
   const int lane = threadIdx.x & 63;
   const int id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = id / groups, g = id - row * groups;
@@ -26,15 +26,15 @@ __global__ __launch_bounds__(256) void search_groups_kernel(const T* __restrict_
   const T* p = logits + (size_t)row * ld;
   const int v0 = g * SEARCH_GROUP;
   float x[8];
-  if (wide && v0 + SEARCH_GROUP <= V) {
+  if (v0 + SEARCH_GROUP <= V) {                              // (wherever the row begins)
     if (sizeof(T) == 2) {
       Frag<T> f;
-      f.load(p + v0 + 8 * lane);
+      load_elements(p + v0 + 8 * lane, 8, f);
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = f.get(i);
     } else {
-      const float4 a = *reinterpret_cast<const float4*>((const float*)p + v0 + 4 * lane), b = *reinterpret_cast<const float4*>((const float*)p + v0 + 256 + 4 * lane);
-      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+      __builtin_memcpy(x, p + v0 + 4 * lane, 16);
+      __builtin_memcpy(x + 4, p + v0 + 256 + 4 * lane, 16);
     }
   } else {
 #pragma unroll
@@ -268,12 +268,11 @@ size_t search_workspace(int B, int K, int V) { return (size_t)B * K * search_gro
 void launch_search_select(int prec, const void* logits, size_t ld, const float* scores, int B, int K, int V, int n, float* out_scores,
                           int32_t* out_rows, int32_t* out_tokens, const SearchAdvance* adv, void* workspace, hipStream_t st) {
   const int groups = search_groups(V);
-  const int wide = (((uintptr_t)logits | ld * (prec ? 2 : 4)) & 15) == 0;
   float2* stat = (float2*)workspace;
   const dim3 grid((unsigned)(((long)B * K * groups + 3) / 4)), threads(64 * std::min(SELECT_WAVES, std::max(4, K)));
   auto go = [&](auto type) {
     using T = decltype(type);
-    hipLaunchKernelGGL(search_groups_kernel<T>, grid, dim3(256), 0, st, (const T*)logits, ld, scores, B * K, V, groups, wide, stat);
+    hipLaunchKernelGGL(search_groups_kernel<T>, grid, dim3(256), 0, st, (const T*)logits, ld, scores, B * K, V, groups, stat);
     if (adv)
       hipLaunchKernelGGL((search_select_kernel<T, true>), dim3(B), threads, 0, st, (const T*)logits, ld, scores, stat, K, V, groups, n, out_scores,
                          out_rows, out_tokens, *adv);
