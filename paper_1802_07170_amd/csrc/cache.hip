@@ -293,25 +293,28 @@ __global__ __launch_bounds__(64 * ATTEND_WAVES) void cache_attend_kernel(AttendA
   fetch_keys(first);
   if (first < bound) {                                       // the queries as operands: [tile][chunk][part][lane]
     Frag<T> raw[GT][EPW];
-    size_t column;
+    auto each = [&](auto f) {                                // f(the query's row, whether there is one, d, the fragment)
 #pragma unroll
-    for (int x = 0; x < GT; ++x) {
-      const bool in = g0 + 16 * x + g < G;
-      const size_t row = row_of(x, column);
-      const T* const qp = (const T*)a.q + (in ? row * a.ldq + column : 0);
+      for (int x = 0; x < GT; ++x) {
+        size_t column;
+        const size_t row = row_of(x, column);
+        const bool in = g0 + 16 * x + g < G;
+        const T* const qp = (const T*)a.q + (in ? row * a.ldq + column : 0);
 #pragma unroll
-      for (int u = 0; u < EPW; ++u) {
-        const int d = 32 * (u * 8 + w) + 8 * q4;
-        if (s.dim >= 8) load_near(qp, d, s.dim, raw[x][u]);
-        else load_elements(qp + d, in ? s.dim - d : 0, raw[x][u]);
+        for (int u = 0; u < EPW; ++u) f(qp, in, 32 * (u * 8 + w) + 8 * q4, raw[x][u]);
       }
+    };
+    if (s.dim >= 8) {
+      each([&](const T* qp, bool, int d, Frag<T>& f) { load_near(qp, d, s.dim, f); });
+      if (s.dim % 8) each([&](const T*, bool, int d, Frag<T>& f) { move_near(d, s.dim, f); });
+    } else {
+      each([&](const T* qp, bool in, int d, Frag<T>& f) { load_elements(qp + d, in ? s.dim - d : 0, f); });
     }
 #pragma unroll
     for (int x = 0; x < GT; ++x)
 #pragma unroll
       for (int u = 0; u < EPW; ++u) {
         Frag<bf16_t> f[QP];
-        if (s.dim >= 8 && s.dim % 8) move_near(32 * (u * 8 + w) + 8 * q4, s.dim, raw[x][u]);
         operand_of(raw[x][u], 32 * (u * 8 + w) + 8 * q4 < s.dim && g0 + 16 * x + g < G, f);
         if (u * 8 + w < E)
 #pragma unroll
